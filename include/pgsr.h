@@ -79,8 +79,10 @@ enum {
 
 /* Pool dtypes.  PGSR_FP8_E4M3 stores K/V as 1-byte OCP E4M3 codes with
  * per-layer scales (pgsr_pool_set_kv_scales); its q, k, v inputs and o
- * outputs are bf16 and attention runs in bf16 on the widened codes. */
-enum { PGSR_F32 = 0, PGSR_BF16 = 1, PGSR_FP8_E4M3 = 2 };
+ * outputs are bf16 and attention runs in bf16 on the widened codes.
+ * PGSR_INT8 stores them as int8 codes with an exponent for each token and KV
+ * head (pgsr_pool_set_kv_exponents), bf16 in and out as well. */
+enum { PGSR_F32 = 0, PGSR_BF16 = 1, PGSR_FP8_E4M3 = 2, PGSR_INT8 = 3 };
 
 /* flags */
 #define PGSR_COMMIT 1u        /* replay: advance each sequence's length by its q_len */
@@ -103,10 +105,11 @@ int pgsr_abi_version(void);
  * NULL means n_blocks-1 .. 0, so pops yield 0, 1, 2, ....  The KV caches are
  * not touched.  workspace (device, nullable) is scratch for split-key partial
  * results, workspace_bytes long (see pgsr_workspace_bytes); NULL disables
- * key splitting.  Supported: dtype PGSR_F32, PGSR_BF16 or PGSR_FP8_E4M3,
- * head_dim 64 or 128, block_size 16, 32 or 64, n_q_heads a multiple of
- * n_kv_heads (bf16 and fp8: at most 32 query heads per KV head, any such
- * group, e.g. 7 for 28 / 4 heads).  An FP8 pool starts with every scale 1.
+ * key splitting.  Supported: dtype PGSR_F32, PGSR_BF16, PGSR_FP8_E4M3 or
+ * PGSR_INT8, head_dim 64 or 128, block_size 16, 32 or 64, n_q_heads a multiple
+ * of n_kv_heads (all but fp32: at most 32 query heads per KV head, any such
+ * group, e.g. 7 for 28 / 4 heads).  An FP8 pool starts with every scale 1; an
+ * int8 pool needs its exponents before the first append.
  * Blocks.
  */
 int pgsr_pool_create(int32_t n_layers, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -130,6 +133,27 @@ int pgsr_pool_create(int32_t n_layers, int32_t n_q_heads, int32_t n_kv_heads, in
  * scale (then nothing changes).  Host only, no device work.
  */
 int pgsr_pool_set_kv_scales(pgsr_pool *pool, const float *k_scales, const float *v_scales);
+
+/*
+ * Int8 KV cache (a storage variant of the same cache; half the bytes of bf16, no
+ * scales to choose): exponents is caller-owned device memory of
+ * n_layers * n_blocks * n_kv_heads * 2 * block_size bytes on a 16-byte boundary,
+ * [layer][block][KV head][K, V][slot], set before the first append of a
+ * PGSR_INT8 pool (a prefill call without it is PGSR_EINVAL) and kept like the
+ * caches.  A token's K row (or V row) of one KV head, head_dim bf16 values x_i
+ * with a = max |x_i| over those that are not NaN, is stored as
+ *   e = clamp(floor(log2 a) - 6, -100, 100)   (a = 0: -100),  byte 127 + e,
+ *   code_i = clamp(rint(x_i 2^-e), -127, 127), ties to even (NaN: 0),
+ * and attention reads code_i 2^e, which bf16 holds exactly: the error is at most
+ * 2^(e-1), 1/128 of a.  Infinities and magnitudes past 127 * 2^100 saturate;
+ * below 2^-101 values read as 0.  A NaN among a token's K and V values of a KV head makes
+ * that key read as NaN (K byte 255, K codes 0): the query rows that see the
+ * token are NaN, and no others.  What is stored for a token depends on its own
+ * values alone, so crops, forks and replays keep the equalities of the other
+ * pools, bit for bit.  PGSR_EINVAL for another pool, NULL or an address off the
+ * boundary.  Host only, no device work.
+ */
+int pgsr_pool_set_kv_exponents(pgsr_pool *pool, void *exponents);
 
 /* Release the host object; device memory is the caller's. NULL is a no-op. */
 int pgsr_pool_destroy(pgsr_pool *pool);
@@ -191,8 +215,8 @@ int pgsr_kv_fork(pgsr_pool *pool, int32_t n, const int32_t *srcs, const int32_t 
  *      head h (KV head h / (n_q_heads / n_kv_heads)), softmax attention over
  *      keys 0 .. p:  o = sum_j softmax_j(softmax_scale * q.k_j) v_j.
  * q, o : [sum S_i][n_q_heads][head_dim];  k, v : [sum S_i][n_kv_heads][head_dim],
- * device, pool dtype (bf16 for an FP8 pool, whose k_j and v_j are the
- * stored codes times the layer's scales), packed in seqs order.  seqs,
+ * device, pool dtype (bf16 for an FP8 or int8 pool, whose k_j and v_j are the
+ * stored codes times their scales), packed in seqs order.  seqs,
  * q_lens: HOST arrays.
  * flags & PGSR_COMMIT adds S_i to each length (set it on the last layer of a
  * step) and sum S_i to *recomputed_tokens (HOST, nullable) -- the count of
@@ -217,7 +241,7 @@ int pgsr_replay_prefill(pgsr_pool *pool, int32_t layer, int32_t n, const int32_t
  * followed by pgsr_replay_prefill(pool, layer, n, seqs, q_lens, ...), but
  * validated together on the host mirror (all-or-nothing across both: the
  * replay is checked against the state the crop leaves) and, where it applies
- * (bf16 pool, at most 16 sequences each with query tokens, at most 512
+ * (no int8 pool, at most 16 sequences each with query tokens, at most 512
  * appended blocks, no kept partial tail block shared with another row), with
  * the crop's device work in the append launch: one launch and one host call
  * fewer between the restore and the replay.  seqs, restore_lens, q_lens: HOST
@@ -289,7 +313,7 @@ int pgsr_pool_set_clock_buffer(pgsr_pool *pool, void *buf, size_t bytes);
 int pgsr_pool_last_clock(pgsr_pool *pool, void *stream, double *ghz, int64_t *cycles, int64_t *ticks);
 
 /*
- * Choice of the prefill attention kernel of bf16 and FP8 pools (Algorithm 1
+ * Choice of the prefill attention kernel of bf16, FP8 and int8 pools (Algorithm 1
  * replay loop, prefill form) for head_dim 128; head_dim 64 always runs the
  * four-wave kernel, and with a workspace calls of at most 32 / G query tokens to a
  * sequence the decode kernel.

@@ -16,6 +16,7 @@ Contents, each following the paper's definitions:
 * :func:`bf16_round` -- round-to-nearest-even to bfloat16, from the format's
   definition (8 significant bits).
 * :func:`e4m3_round` -- rounding to FP8 E4M3 for the FP8 KV pool (F1, F2).
+* :func:`int8_row` -- codes and exponents of the int8 KV pool (I1, I2).
 * :func:`stacked_layers` -- the stacked random-init layer F used by the 70B-like
   workload (a reading: the paper defines no layer).
 * :func:`recomputed_transitions`, :func:`replay_gain` -- Corollary 1.
@@ -53,6 +54,15 @@ precision; the variant halves the bytes a decode step reads):
      (bf16 from the projection) is stored as the code e4m3(fp32(x / scale)),
      with fp32 the correctly rounded quotient, and read back as code * scale;
      attention runs on the read-back values.
+
+Readings of the int8 KV cache variant (a scale that needs no choosing):
+  I1 a token's K row or V row of one KV head, head_dim bf16 values x_i, has the
+     exponent e = clamp(floor(log2 a) - 6, -100, 100), a the largest |x_i| that
+     is not NaN (e = -100 when there is none or it is 0), and the codes
+     clamp(rint(x_i / 2^e), -127, 127), ties to even; it reads back as
+     code * 2^e (:func:`int8_row`), so infinities saturate;
+  I2 a NaN among a token's K and V values of a KV head makes its K row read as
+     NaN; NaN values of V read as 0.
 """
 from __future__ import annotations
 
@@ -173,6 +183,26 @@ def e4m3_round(x: np.ndarray) -> np.ndarray:
     return np.where(np.isnan(x), np.nan, np.copysign(r, x))
 
 
+def int8_row(x: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
+    """Codes [..., d] and exponents [...] (int64) of rows of the last axis, from
+    the definition (I1)."""
+    x = np.asarray(x, dtype=np.float64)
+    a = np.where(np.isnan(x), 0.0, np.abs(x)).max(-1)
+    e = np.full(a.shape, -100, np.int64)
+    at = np.isfinite(a) & (a > 0)
+    e[at] = np.frexp(a[at])[1] - 1 - 6               # a = m 2^k with 1/2 <= m < 1
+    e[np.isinf(a)] = 100
+    e = np.clip(e, -100, 100)
+    codes = np.clip(np.rint(np.ldexp(np.where(np.isnan(x), 0.0, x), -e[..., None])), -127, 127)
+    return codes.astype(np.int64), e
+
+
+def int8_read(x: np.ndarray) -> np.ndarray:
+    """What rows of the last axis read back as (I1)."""
+    codes, e = int8_row(x)
+    return np.ldexp(codes.astype(np.float64), e[..., None])
+
+
 def _cdiv(a: int, b: int) -> int:
     return -(-a // b)
 
@@ -190,8 +220,10 @@ class PoolModel:
 
     def __init__(self, n_blocks: int, max_seqs: int, max_blocks: int, block_size: int,
                  init_free_order: Optional[Sequence[int]] = None,
-                 n_layers: int = 0, n_kv_heads: int = 0, head_dim: int = 0, kv_fp8: bool = False):
+                 n_layers: int = 0, n_kv_heads: int = 0, head_dim: int = 0, kv_fp8: bool = False,
+                 kv_int8: bool = False):
         self.B = block_size
+        self.kv_int8 = kv_int8               # store what is read back (I1, I2)
         self.kv_fp8 = kv_fp8                 # store codes (F1, F2); scales per layer
         self.k_scales = np.ones(max(n_layers, 1))
         self.v_scales = np.ones(max(n_layers, 1))
@@ -345,6 +377,9 @@ class PoolModel:
         if self.kv_fp8:
             k = self.quantize(k, self.k_scales[layer])
             v = self.quantize(v, self.v_scales[layer])
+        elif self.kv_int8:
+            nan = (np.isnan(k) | np.isnan(v)).any(-1, keepdims=True)
+            k, v = np.where(nan, np.nan, int8_read(k)), int8_read(v)
         for t in range(k.shape[0]):
             b, o = self.slot(seq, start + t)
             self.kdata[layer, b, o] = k[t]

@@ -16,7 +16,7 @@ LIB_PATH = os.environ.get("PGSR_LIB") or os.path.join(_PKG, "lib", "libpgsr.so")
 
 OK, EINVAL, ERANGE, ENOMEM, EUNSUPPORTED, EHIP, ENOENT = range(7)
 STATIC_SCRATCH_BYTES = 64 << 20      # PGSR_STATIC_SCRATCH_BYTES
-F32, BF16, FP8_E4M3 = 0, 1, 2
+F32, BF16, FP8_E4M3, INT8 = 0, 1, 2, 3
 COMMIT, POISON = 1, 2
 
 EXPORTS = (
@@ -26,6 +26,7 @@ EXPORTS = (
     "pgsr_restore_replay_prefill",
     "pgsr_full_reset_prefill", "pgsr_gemm_bf16", "pgsr_gemm_bf16_multi", "pgsr_gemm_silu_bf16",
     "pgsr_pool_enable_timing", "pgsr_pool_last_times", "pgsr_pool_set_kv_scales",
+    "pgsr_pool_set_kv_exponents",
     "pgsr_pool_set_prefill_kernel", "pgsr_pool_set_clock_buffer", "pgsr_pool_last_clock",
     "pgsr_graph_create", "pgsr_graph_destroy", "pgsr_graph_append", "pgsr_graph_size",
     "pgsr_graph_session_length", "pgsr_graph_kv_length_after", "pgsr_graph_locate_source",
@@ -96,6 +97,8 @@ def _load() -> ctypes.CDLL:
                                                ctypes.POINTER(i64), P]
     lib.pgsr_pool_set_kv_scales.restype = ctypes.c_int
     lib.pgsr_pool_set_kv_scales.argtypes = [P, P, P]
+    lib.pgsr_pool_set_kv_exponents.restype = ctypes.c_int
+    lib.pgsr_pool_set_kv_exponents.argtypes = [P, P]
     lib.pgsr_pool_enable_timing.restype = ctypes.c_int
     lib.pgsr_pool_enable_timing.argtypes = [P, ctypes.c_int]
     lib.pgsr_pool_last_times.restype = ctypes.c_int

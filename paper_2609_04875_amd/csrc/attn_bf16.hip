@@ -76,13 +76,13 @@ struct Ids {
   __device__ int32_t get(int i) const { return i == 0 ? v0 : i == 1 ? v1 : i == 2 ? v2 : v3; }
 };
 
-template <int D, int NW, int B, bool F8>
+template <int D, int NW, int B, int CK>
 __global__ void __launch_bounds__(NW * 64, 2)
 attn_bf16_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t* __restrict__ qg_,
-                 const std::conditional_t<F8, uint8_t, uint16_t>* __restrict__ kc,
-                 const std::conditional_t<F8, uint8_t, uint16_t>* __restrict__ vc,
+                 const cache_elem<CK>* __restrict__ kc,
+                 const cache_elem<CK>* __restrict__ vc,
                  uint16_t* __restrict__ og) {
-  using Raw = std::conditional_t<F8, u32x2, u32x4>;   // 8 cache elements
+  using Raw = std::conditional_t<CK == kCacheBf16, u32x4, u32x2>;   // 8 cache elements
   constexpr int KT = kKT;
   constexpr int KB = KT / B;               // blocks per key tile
   constexpr int KLD = D + 8;               // LDS row stride of the K tile (elements)
@@ -180,6 +180,8 @@ attn_bf16_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t*
   };
 
   Raw kreg[CPT], vreg[CPT];
+  uint32_t kexp[CK == kCacheInt8 ? CPT : 1];       // int8: a K chunk's exponent, a V chunk's eight
+  u32x2 vexp[CK == kCacheInt8 ? CPT : 1];
   auto load_tile = [&](const Ids& ids) {
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
@@ -187,20 +189,31 @@ attn_bf16_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t*
       const int64_t base = (head_base + (int64_t)ids.get(chunk_blk(i)) * hkv) * (B * D);
       kreg[i] = *(const Raw*)(kc + base + (in / (D / 8)) * D + (in % (D / 8)) * 8);
       vreg[i] = *(const Raw*)(vc + base + (in / (B / 8)) * B + (in % (B / 8)) * 8);
+      if constexpr (CK == kCacheInt8) {
+        const uint8_t* xp = a.kv_exps + (head_base + (int64_t)ids.get(chunk_blk(i)) * hkv) * (2 * B);
+        kexp[i] = xp[in / (D / 8)];
+        vexp[i] = *(const u32x2*)(xp + B + (in % (B / 8)) * 8);
+      }
     }
   };
-  auto as_bf16 = [](const Raw& x) {
-    if constexpr (F8) return widen_fp8(x);
-    else return x;
+  auto k_bf16 = [&](int i) {
+    if constexpr (CK == kCacheFp8) return widen_fp8(kreg[i]);
+    else if constexpr (CK == kCacheInt8) return widen_int8(kreg[i], __uint_as_float(kexp[i] << 23));
+    else return kreg[i];
+  };
+  auto v_bf16 = [&](int i) {
+    if constexpr (CK == kCacheFp8) return widen_fp8(vreg[i]);
+    else if constexpr (CK == kCacheInt8) return widen_int8(vreg[i], vexp[i]);
+    else return vreg[i];
   };
   auto store_tile = [&](int buf, int kb) {
     const bool tail = kb + KT > kv_len;   // V slots at or past kv_len must read as 0
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
       const int blk = chunk_blk(i), in = chunk_in(i);
-      *(u32x4*)&k_lds[buf][(blk * B + in / (D / 8)) * KLD + (in % (D / 8)) * 8] = as_bf16(kreg[i]);
+      *(u32x4*)&k_lds[buf][(blk * B + in / (D / 8)) * KLD + (in % (D / 8)) * 8] = k_bf16(i);
       const int dd = in / (B / 8), key0 = blk * B + (in % (B / 8)) * 8;
-      u32x4 val = as_bf16(vreg[i]);
+      u32x4 val = v_bf16(i);
       if (tail) {
         const int pos0 = kb + key0;
         if (pos0 >= kv_len) val = u32x4{0, 0, 0, 0};
@@ -474,21 +487,21 @@ __global__ void __launch_bounds__(256) split_combine_kernel(AttnArgs a, TO* __re
 
 int attn_bf16_tile_tokens(int, int group) { return kNW * (32 / group); }
 
-template <int D, int B, bool F8>
+template <int D, int B, int CK>
 static void launch_d_b(const AttnArgs& a, hipStream_t s) {
-  using CT = std::conditional_t<F8, uint8_t, uint16_t>;
+  using CT = cache_elem<CK>;
   dim3 grid(a.n_tiles * a.n_kv_heads * a.n_splits);
-  hipLaunchKernelGGL((attn_bf16_kernel<D, kNW, B, F8>), grid, dim3(kNW * 64), 0, s, a, a.tables,
+  hipLaunchKernelGGL((attn_bf16_kernel<D, kNW, B, CK>), grid, dim3(kNW * 64), 0, s, a, a.tables,
                      (const uint16_t*)a.q, (const CT*)a.k_cache, (const CT*)a.v_cache,
                      (uint16_t*)a.o);
 }
 
-template <int D, bool F8>
+template <int D, int CK>
 static hipError_t launch_d(const AttnArgs& a, hipStream_t s) {
   switch (a.block_size) {
-    case 16: launch_d_b<D, 16, F8>(a, s); break;
-    case 32: launch_d_b<D, 32, F8>(a, s); break;
-    case 64: launch_d_b<D, 64, F8>(a, s); break;
+    case 16: launch_d_b<D, 16, CK>(a, s); break;
+    case 32: launch_d_b<D, 32, CK>(a, s); break;
+    case 64: launch_d_b<D, 64, CK>(a, s); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
@@ -522,18 +535,16 @@ hipError_t launch_split_combine(const AttnArgs& a, bool f32_out, int group, hipS
   return hipGetLastError();
 }
 
-hipError_t launch_attn_bf16(const AttnArgs& a, hipStream_t s) {
+template <int CK>
+static hipError_t launch_kind(const AttnArgs& a, hipStream_t s) {
   if (a.n <= 0 || a.n_tiles <= 0) return hipSuccess;
-  if (a.head_dim == 128) return launch_d<128, false>(a, s);
-  if (a.head_dim == 64) return launch_d<64, false>(a, s);
+  if (a.head_dim == 128) return launch_d<128, CK>(a, s);
+  if (a.head_dim == 64) return launch_d<64, CK>(a, s);
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_attn_fp8(const AttnArgs& a, hipStream_t s) {
-  if (a.n <= 0 || a.n_tiles <= 0) return hipSuccess;
-  if (a.head_dim == 128) return launch_d<128, true>(a, s);
-  if (a.head_dim == 64) return launch_d<64, true>(a, s);
-  return hipErrorInvalidValue;
-}
+hipError_t launch_attn_bf16(const AttnArgs& a, hipStream_t s) { return launch_kind<kCacheBf16>(a, s); }
+hipError_t launch_attn_fp8(const AttnArgs& a, hipStream_t s) { return launch_kind<kCacheFp8>(a, s); }
+hipError_t launch_attn_int8(const AttnArgs& a, hipStream_t s) { return launch_kind<kCacheInt8>(a, s); }
 
 }  // namespace pgsr

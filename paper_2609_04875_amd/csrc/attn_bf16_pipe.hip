@@ -68,13 +68,13 @@ constexpr int kPKT = 64;        // keys per tile
 constexpr int kPBuf = 3;        // LDS tile buffers
 constexpr float kPSlack = 8.f;  // lazy rescale threshold, log2 units
 
-template <int B, int NW, bool F8>
+template <int B, int NW, int CK>
 __global__ void __launch_bounds__(NW * 64, 1)
 attn_bf16_pipe_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t* __restrict__ qg_,
-                      const std::conditional_t<F8, uint8_t, uint16_t>* __restrict__ kc,
-                      const std::conditional_t<F8, uint8_t, uint16_t>* __restrict__ vc,
+                      const cache_elem<CK>* __restrict__ kc,
+                      const cache_elem<CK>* __restrict__ vc,
                       uint16_t* __restrict__ og) {
-  using Raw = std::conditional_t<F8, u32x2, u32x4>;   // 8 cache elements
+  using Raw = std::conditional_t<CK == kCacheBf16, u32x4, u32x2>;   // 8 cache elements
   constexpr int D = 128, QB = kPQB, KT = kPKT;
   constexpr int KB = KT / B;               // blocks per key tile
   constexpr int KLD = D + 8;               // LDS row stride of the K tile (elements)
@@ -185,9 +185,17 @@ attn_bf16_pipe_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint
     voff[i] = (in / (B / 8)) * B + (in % (B / 8)) * 8;
   }
   Raw kreg[CPT], vreg[CPT];
-  auto as_bf16 = [](const Raw& x) {
-    if constexpr (F8) return widen_fp8(x);
-    else return x;
+  uint32_t kexp[CK == kCacheInt8 ? CPT : 1];       // int8: a K chunk's exponent, a V chunk's eight
+  u32x2 vexp[CK == kCacheInt8 ? CPT : 1];
+  auto k_bf16 = [&](int i) {
+    if constexpr (CK == kCacheFp8) return widen_fp8(kreg[i]);
+    else if constexpr (CK == kCacheInt8) return widen_int8(kreg[i], __uint_as_float(kexp[i] << 23));
+    else return kreg[i];
+  };
+  auto v_bf16 = [&](int i) {
+    if constexpr (CK == kCacheFp8) return widen_fp8(vreg[i]);
+    else if constexpr (CK == kCacheInt8) return widen_int8(vreg[i], vexp[i]);
+    else return vreg[i];
   };
   auto load_tile = [&](int ids) {
 #pragma unroll
@@ -196,6 +204,11 @@ attn_bf16_pipe_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint
       const int64_t base = (head_base + (int64_t)id * hkv) * (B * D);
       kreg[i] = *(const Raw*)((kc + base) + koff[i]);
       vreg[i] = *(const Raw*)((vc + base) + voff[i]);
+      if constexpr (CK == kCacheInt8) {
+        const uint8_t* xp = a.kv_exps + (head_base + (int64_t)id * hkv) * (2 * B);
+        kexp[i] = xp[chunk_in(i) / (D / 8)];
+        vexp[i] = *(const u32x2*)(xp + B + (chunk_in(i) % (B / 8)) * 8);
+      }
     }
   };
   auto store_tile = [&](int buf, int kb) {
@@ -203,9 +216,9 @@ attn_bf16_pipe_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
       const int blk = chunk_blk(i), in = chunk_in(i);
-      *(u32x4*)&k_lds[buf][(blk * B + in / (D / 8)) * KLD + (in % (D / 8)) * 8] = as_bf16(kreg[i]);
+      *(u32x4*)&k_lds[buf][(blk * B + in / (D / 8)) * KLD + (in % (D / 8)) * 8] = k_bf16(i);
       const int dd = in / (B / 8), key0 = blk * B + (in % (B / 8)) * 8;
-      u32x4 val = as_bf16(vreg[i]);
+      u32x4 val = v_bf16(i);
       if (tail) val = zero_tail(val, kb + key0, kv_len);   // selects only: no per-lane branch
       *(u32x4*)&v_lds[buf][dd * VLD + key0] = val;
     }
@@ -522,30 +535,35 @@ bool attn_bf16_pipe_eligible(int head_dim, int group) { return head_dim == 128 &
 
 int attn_bf16_pipe_tile_tokens(int group, int waves) { return waves * kPQB * (32 / group); }
 
-template <int B, int NW, bool F8>
+template <int B, int NW, int CK>
 static void launch_p(const AttnArgs& a, hipStream_t s) {
-  using CT = std::conditional_t<F8, uint8_t, uint16_t>;
-  hipLaunchKernelGGL((attn_bf16_pipe_kernel<B, NW, F8>), dim3(a.n_tiles * a.n_kv_heads * a.n_splits), dim3(NW * 64), 0,
+  using CT = cache_elem<CK>;
+  hipLaunchKernelGGL((attn_bf16_pipe_kernel<B, NW, CK>), dim3(a.n_tiles * a.n_kv_heads * a.n_splits), dim3(NW * 64), 0,
                      s, a, a.tables, (const uint16_t*)a.q, (const CT*)a.k_cache, (const CT*)a.v_cache,
                      (uint16_t*)a.o);
 }
 
-template <int NW, bool F8>
+template <int NW, int CK>
 static hipError_t launch_p_b(const AttnArgs& a, hipStream_t s) {
   switch (a.block_size) {
-    case 16: launch_p<16, NW, F8>(a, s); break;
-    case 32: launch_p<32, NW, F8>(a, s); break;
-    case 64: launch_p<64, NW, F8>(a, s); break;
+    case 16: launch_p<16, NW, CK>(a, s); break;
+    case 32: launch_p<32, NW, CK>(a, s); break;
+    case 64: launch_p<64, NW, CK>(a, s); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
 }
 
-hipError_t launch_attn_bf16_pipe(const AttnArgs& a, int waves, bool fp8, hipStream_t s) {
+hipError_t launch_attn_bf16_pipe(const AttnArgs& a, int waves, int cache, hipStream_t s) {
   if (a.n <= 0 || a.n_tiles <= 0) return hipSuccess;
   if (!attn_bf16_pipe_eligible(a.head_dim, a.n_q_heads / a.n_kv_heads)) return hipErrorInvalidValue;
-  if (waves == 8) return fp8 ? launch_p_b<8, true>(a, s) : launch_p_b<8, false>(a, s);
-  if (waves == 4 && fp8) return launch_p_b<4, true>(a, s);   // bf16 calls that leave CUs idle take other kernels
+  if (waves == 8)
+    return cache == kCacheFp8    ? launch_p_b<8, kCacheFp8>(a, s)
+           : cache == kCacheInt8 ? launch_p_b<8, kCacheInt8>(a, s)
+                                 : launch_p_b<8, kCacheBf16>(a, s);
+  // bf16 calls that leave CUs idle take other kernels
+  if (waves == 4 && cache == kCacheFp8) return launch_p_b<4, kCacheFp8>(a, s);
+  if (waves == 4 && cache == kCacheInt8) return launch_p_b<4, kCacheInt8>(a, s);
   return hipErrorInvalidValue;
 }
 

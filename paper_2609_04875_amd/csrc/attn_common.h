@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 namespace pgsr {
 namespace {
@@ -56,6 +57,61 @@ __device__ inline u32x4 widen_fp8(u32x2 w) {
   for (int h = 0; h < 2; ++h) {
     r[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[h], 1.0f, false));
     r[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[h], 1.0f, true));
+  }
+  return r;
+}
+
+// How a pool stores K and V: bf16 values, E4M3 codes under a scale per layer, or
+// int8 codes with an exponent byte (127 + e: value = code * 2^e) for each token and
+// KV head.
+constexpr int kCacheBf16 = 0, kCacheFp8 = 1, kCacheInt8 = 2;
+template <int CK>
+using cache_elem = std::conditional_t<CK == kCacheBf16, uint16_t, uint8_t>;
+
+// 2^e of the exponent byte i (0..3) of w; 0 for byte 0, infinity for byte 255 (a key
+// that reads as NaN: its codes are 0).
+template <int I>
+__device__ inline float exp_byte(uint32_t w) {
+  if constexpr (I < 3) w <<= 23 - 8 * I;
+  else w >>= 1;
+  return __uint_as_float(w & 0x7F800000u);
+}
+
+// bf16 values a, b (exact in their upper halves) as a pair
+__device__ inline uint32_t pair_of(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+
+// Eight int8 codes as the bf16 values code * s, s a power of two: at most seven
+// significant bits, so every step is exact.  The form without s gives the codes.
+__device__ inline u32x4 widen_int8(u32x2 w, float s) {
+  u32x4 r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int x = (int)w[h];
+    r[2 * h] = pair_of((float)(int8_t)x * s, (float)(int8_t)(x >> 8) * s);
+    r[2 * h + 1] = pair_of((float)(int8_t)(x >> 16) * s, (float)(x >> 24) * s);
+  }
+  return r;
+}
+__device__ inline u32x4 widen_int8(u32x2 w) {
+  u32x4 r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int x = (int)w[h];
+    r[2 * h] = pair_of((float)(int8_t)x, (float)(int8_t)(x >> 8));
+    r[2 * h + 1] = pair_of((float)(int8_t)(x >> 16), (float)(x >> 24));
+  }
+  return r;
+}
+// The same with a power of two for each code, from eight exponent bytes.
+__device__ inline u32x4 widen_int8(u32x2 w, u32x2 e) {
+  u32x4 r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int x = (int)w[h];
+    r[2 * h] = pair_of((float)(int8_t)x * exp_byte<0>(e[h]), (float)(int8_t)(x >> 8) * exp_byte<1>(e[h]));
+    r[2 * h + 1] = pair_of((float)(int8_t)(x >> 16) * exp_byte<2>(e[h]), (float)(x >> 24) * exp_byte<3>(e[h]));
   }
   return r;
 }

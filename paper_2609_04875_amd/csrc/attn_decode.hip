@@ -51,20 +51,21 @@ namespace {
 constexpr int kDecKT = 32;          // keys per tile
 constexpr float kDecSlack = 8.f;    // lazy rescale threshold, log2 units
 
-template <int D, int B, bool F8>
+template <int D, int B, int CK>
 __global__ void __launch_bounds__(256, 2)
 attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t* __restrict__ qg_,
-                   const std::conditional_t<F8, uint8_t, uint16_t>* __restrict__ kc,
-                   const std::conditional_t<F8, uint8_t, uint16_t>* __restrict__ vc,
+                   const cache_elem<CK>* __restrict__ kc, const cache_elem<CK>* __restrict__ vc,
                    uint16_t* __restrict__ og) {
   constexpr int KT = kDecKT;
+  constexpr bool kByte = CK != kCacheBf16;       // one-byte codes
+  constexpr bool I8 = CK == kCacheInt8;
   constexpr int NDS = D / 16;                    // S^T MFMA steps over d
   constexpr int NDB = D / 32;                    // 32-row blocks of O^T
-  constexpr int NK = F8 ? NDS / 2 : NDS;         // 16-byte K loads per tile
-  constexpr int NV = F8 ? NDB : 2 * NDB;         // 16-byte V loads per tile
-  constexpr int EK = F8 ? 16 : 8;                // cache elements per 16-byte load
+  constexpr int NK = kByte ? NDS / 2 : NDS;         // 16-byte K loads per tile
+  constexpr int NV = kByte ? NDB : 2 * NDB;         // 16-byte V loads per tile
+  constexpr int EK = kByte ? 16 : 8;                // cache elements per 16-byte load
   static_assert(B % 16 == 0, "a 16-key group never straddles two blocks");
-  constexpr bool kQLds = !F8 && D == 128;        // Q^T in LDS instead of registers
+  constexpr bool kQLds = !kByte && D == 128;        // Q^T in LDS instead of registers
   constexpr int QLD = D + 8;                     // padded LDS row of Q (elements)
   __shared__ __attribute__((aligned(16))) uint16_t q_lds[kQLds ? 4 * 32 * QLD : 1];
 
@@ -142,24 +143,37 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
     const auto* vp = vc + ((head_base + (int64_t)idv * hkv) * D + r) * B + v_key(kb) % B;
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
-      const int db = F8 ? c : c / 2, ks = F8 ? 0 : c % 2;
+      const int db = kByte ? c : c / 2, ks = kByte ? 0 : c % 2;
       const u32x4* at = (const u32x4*)(vp + (int64_t)db * 32 * B + 8 * ks);
-      if constexpr (F8 && B == 16) vr[c] = __builtin_nontemporal_load(at);
+      if constexpr (kByte && B == 16) vr[c] = __builtin_nontemporal_load(at);
       else vr[c] = *at;
     }
   };
+  auto widen = [](u32x2 w) {
+    if constexpr (I8) return widen_int8(w);
+    else return widen_fp8(w);
+  };
+  // int8: exponents of this lane's 16 keys, K and V
+  u32x4 ke, ve;
+  auto load_e = [&](int kb, int idv) {
+    if constexpr (I8) {
+      const uint8_t* xp = a.kv_exps + (head_base + (int64_t)idv * hkv) * (2 * B) + v_key(kb) % B;
+      ke = *(const u32x4*)xp;
+      ve = *(const u32x4*)(xp + B);
+    }
+  };
   auto k_operand = [&](const u32x4 (&k)[NK], int ds) {
-    if constexpr (F8) {
+    if constexpr (kByte) {
       const u32x4 w = k[ds / 2];
-      return __builtin_bit_cast(bf16x8, widen_fp8(ds % 2 ? u32x2{w[2], w[3]} : u32x2{w[0], w[1]}));
+      return __builtin_bit_cast(bf16x8, widen(ds % 2 ? u32x2{w[2], w[3]} : u32x2{w[0], w[1]}));
     } else {
       return __builtin_bit_cast(bf16x8, k[ds]);
     }
   };
   auto v_operand = [&](const u32x4 (&v)[NV], int ks, int db) {
-    if constexpr (F8) {
+    if constexpr (kByte) {
       const u32x4 w = v[db];
-      return widen_fp8(ks ? u32x2{w[2], w[3]} : u32x2{w[0], w[1]});
+      return widen(ks ? u32x2{w[2], w[3]} : u32x2{w[0], w[1]});
     } else {
       return v[2 * db + ks];
     }
@@ -182,6 +196,7 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
   const int n_kt = (key_hi - key_lo + KT - 1) / KT;
   load_k(key_lo, k_id(key_lo));
   load_v(key_lo, v_id(key_lo));
+  load_e(key_lo, v_id(key_lo));
   int idk_n = 0, idv_n = 0;
   if (n_kt > 1) {
     idk_n = k_id(key_lo + KT);
@@ -200,8 +215,21 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(kcur, ds), q_operand(ds), s, 0, 0, 0);
 #pragma unroll
     for (int c = 0; c < NV; ++c) vcur[c] = vr[c];
+    u32x4 vecur{};
+    if constexpr (I8) {
+      // S in units of each key's step: times 2^e of the key
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        s[4 * w + 0] *= exp_byte<0>(ke[w]);
+        s[4 * w + 1] *= exp_byte<1>(ke[w]);
+        s[4 * w + 2] *= exp_byte<2>(ke[w]);
+        s[4 * w + 3] *= exp_byte<3>(ke[w]);
+      }
+      vecur = ve;
+    }
     if (more) {
       load_v(kb + KT, idv_n);
+      load_e(kb + KT, idv_n);
       if (j + 2 < n_kt) {
         idk_n = k_id(kb + 2 * KT);
         idv_n = v_id(kb + 2 * KT);
@@ -234,6 +262,26 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
       ps1 = __builtin_amdgcn_fdot2_f32_bf16(p2[1], kOnes, ps1, false);
       ps0 = __builtin_amdgcn_fdot2_f32_bf16(p2[2], kOnes, ps0, false);
       ps1 = __builtin_amdgcn_fdot2_f32_bf16(p2[3], kOnes, ps1, false);
+      if constexpr (I8) {
+        // the weights of the PV product carry 2^e of V's key; the rounding of P is
+        // the same, a power of two apart.  Keys past the end have no exponent.
+        float e8[8];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const uint32_t x = vecur[2 * ks + w];
+          e8[4 * w + 0] = exp_byte<0>(x);
+          e8[4 * w + 1] = exp_byte<1>(x);
+          e8[4 * w + 2] = exp_byte<2>(x);
+          e8[4 * w + 3] = exp_byte<3>(x);
+        }
+        if (kb + KT > kv_len) {
+#pragma unroll
+          for (int t = 0; t < 8; ++t) e8[t] = kb + 16 * hh + 8 * ks + t < kv_len ? e8[t] : 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < 8; ++t) p8[t] *= e8[t];
+        pb[ks] = __builtin_convertvector(p8, bf16x8);
+      }
     }
     l = fmaf(l, alpha, ps0 + ps1);
     if (__ballot(bump)) {
@@ -279,20 +327,20 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
   }
 }
 
-template <int D, int B, bool F8>
+template <int D, int B, int CK>
 void launch_dec(const AttnArgs& a, hipStream_t s) {
-  using CT = std::conditional_t<F8, uint8_t, uint16_t>;
-  hipLaunchKernelGGL((attn_decode_kernel<D, B, F8>), dim3((unsigned)((a.n_tiles + 3) / 4)), dim3(256), 0, s, a,
+  using CT = cache_elem<CK>;
+  hipLaunchKernelGGL((attn_decode_kernel<D, B, CK>), dim3((unsigned)((a.n_tiles + 3) / 4)), dim3(256), 0, s, a,
                      a.tables, (const uint16_t*)a.q, (const CT*)a.k_cache, (const CT*)a.v_cache,
                      (uint16_t*)a.o);
 }
 
-template <int D, bool F8>
+template <int D, int CK>
 hipError_t launch_dec_d(const AttnArgs& a, hipStream_t s) {
   switch (a.block_size) {
-    case 16: launch_dec<D, 16, F8>(a, s); break;
-    case 32: launch_dec<D, 32, F8>(a, s); break;
-    case 64: launch_dec<D, 64, F8>(a, s); break;
+    case 16: launch_dec<D, 16, CK>(a, s); break;
+    case 32: launch_dec<D, 32, CK>(a, s); break;
+    case 64: launch_dec<D, 64, CK>(a, s); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
@@ -302,11 +350,18 @@ hipError_t launch_dec_d(const AttnArgs& a, hipStream_t s) {
 
 int attn_decode_keys_per_tile() { return kDecKT; }
 
-hipError_t launch_attn_decode(const AttnArgs& a, bool fp8, hipStream_t s) {
-  if (a.n <= 0) return hipSuccess;
-  if (a.head_dim == 128) return fp8 ? launch_dec_d<128, true>(a, s) : launch_dec_d<128, false>(a, s);
-  if (a.head_dim == 64) return fp8 ? launch_dec_d<64, true>(a, s) : launch_dec_d<64, false>(a, s);
+template <int CK>
+static hipError_t launch_dec_kind(const AttnArgs& a, hipStream_t s) {
+  if (a.head_dim == 128) return launch_dec_d<128, CK>(a, s);
+  if (a.head_dim == 64) return launch_dec_d<64, CK>(a, s);
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_attn_decode(const AttnArgs& a, int cache, hipStream_t s) {
+  if (a.n <= 0) return hipSuccess;
+  return cache == kCacheFp8    ? launch_dec_kind<kCacheFp8>(a, s)
+         : cache == kCacheInt8 ? launch_dec_kind<kCacheInt8>(a, s)
+                               : launch_dec_kind<kCacheBf16>(a, s);
 }
 
 }  // namespace pgsr

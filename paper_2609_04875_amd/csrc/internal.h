@@ -74,6 +74,7 @@ struct PoisonArgs {
   int32_t max_bps, n_layers, n_blocks, n_kv_heads, block_size, head_dim, elem_bytes;
   int32_t top_before;
   int32_t n_freed;
+  uint8_t* kv_exps;    // int8 pools: their exponents are poisoned too
   int32_t n;
   CropEntry e[kMaxSeqsPerLaunch];
 };
@@ -130,6 +131,7 @@ struct AppendArgs {
   int32_t n;
   int32_t n_items;
   AppendEntry e[kMaxSeqsPerLaunch];
+  uint8_t* kv_exps;    // int8 cache: exponent bytes [layer][block][KV head][K, V][slot], else null
 };
 
 // Restore + reserve + append in one launch (no copy-on-write, no poisoning):
@@ -205,6 +207,7 @@ struct AttnArgs {
   uint64_t* clk;
   int32_t clk_n;
   AttnEntry e[kMaxSeqsPerLaunch];
+  const uint8_t* kv_exps;   // int8 cache: exponent bytes [layer][block][KV head][K, V][slot]
 };
 
 // ------------------------------------------------------------- sampling -- //
@@ -234,18 +237,22 @@ hipError_t launch_crop(const CropArgs& a, hipStream_t s);
 hipError_t launch_poison(const PoisonArgs& a, hipStream_t s);
 hipError_t launch_fork(const ForkArgs& a, hipStream_t s);
 hipError_t launch_append(const AppendArgs& a, int elem_bytes, hipStream_t s);
+// The copy-on-write part of an append (nothing where no entry has a shared tail),
+// and the append of an int8 pool, which quantises a row of each token and KV head.
+hipError_t launch_cow(const AppendArgs& a, int elem_bytes, hipStream_t s);
+hipError_t launch_append_int8(const AppendArgs& a, hipStream_t s);
 // False when the fused launch does not cover this geometry (the caller then
 // launches crop and append separately).
 bool fused_append_supported(int block_size, int head_dim);
 hipError_t launch_fused_append(const FusedAppendArgs& a, int elem_bytes, hipStream_t s);
 hipError_t launch_attn_f32(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_bf16(const AttnArgs& a, hipStream_t s);
-// Software-pipelined prefill for head_dim 128, bf16 and FP8 pools: 32 query
+// Software-pipelined prefill for head_dim 128, every cache but fp32: 32 query
 // rows per wave, one workgroup per CU of 8 waves (two per SIMD) or, for calls
 // that leave CUs idle, 4.
 bool attn_bf16_pipe_eligible(int head_dim, int group);
 int attn_bf16_pipe_tile_tokens(int group, int waves);
-hipError_t launch_attn_bf16_pipe(const AttnArgs& a, int waves, bool fp8, hipStream_t s);
+hipError_t launch_attn_bf16_pipe(const AttnArgs& a, int waves, int cache, hipStream_t s);
 // The same tiles and bits with one wave per SIMD holding 64 query rows and
 // global->LDS tile loads: 16-token blocks, pools whose layer-head block range
 // fits 32-bit byte offsets, sequences of up to 130816 keys (a workgroup's
@@ -261,10 +268,13 @@ hipError_t launch_attn_bf16_narrow(const AttnArgs& a, int waves, hipStream_t s);
 // Same kernel over an FP8 E4M3 cache: codes widen to bf16 exactly on the way
 // into LDS; the K scale is in scale_log2, the V scale in o_scale.
 hipError_t launch_attn_fp8(const AttnArgs& a, hipStream_t s);
+// And over an int8 cache: each code times its token's power of two is a bf16 value.
+hipError_t launch_attn_int8(const AttnArgs& a, hipStream_t s);
 // Decode attention (every sequence of the launch has at most 32 / G query
 // tokens): one wave per (sequence, KV head, split) gathering MFMA operands from
 // the cache without LDS; with n_splits > 1 it writes split partials.
-hipError_t launch_attn_decode(const AttnArgs& a, bool fp8, hipStream_t s);
+// `cache`: kCacheBf16, kCacheFp8 or kCacheInt8 (attn_common.h).
+hipError_t launch_attn_decode(const AttnArgs& a, int cache, hipStream_t s);
 int attn_decode_keys_per_tile();
 // Merge split-key partials into O (bf16, or fp32 for fp32 pools), splits in
 // increasing order, `group` (8 or 16) of them to a round trip.

@@ -1,0 +1,195 @@
+// Append of an int8 KV pool: each token's K row and V row of a KV head (head_dim
+// bf16 values) becomes int8 codes under a power of two of its own.
+//
+// For a row x with a = max |x_i| (its NaN left out):
+//   e = clamp(floor(log2 a) - 6, -100, 100)  (a = 0: -100),
+//   code_i = clamp(rint(x_i 2^-e), -127, 127), ties to even; NaN: 0,
+// and code_i 2^e is read back.  floor(log2 a) is the exponent field of a, so
+// 64 <= max |code| <= 127 inside the clamp, and x_i 2^-e is exact: codes and
+// exponents are integers defined bit for bit.  A power of two and not a / 127 makes
+// code 2^e a bf16 value (seven significant bits), so the attention kernels run on
+// exactly what is stored; it costs half a bit of the eight on average.  One token and
+// not a run of tokens to an exponent, because a crop keeps any number of tokens:
+// what is stored for a kept token must not depend on tokens that it forgets, nor on
+// how the tokens were batched (replay from the crop equals the full reset, bit for
+// bit).  The exponents cost 1/64 to 1/128 of the codes' bytes.
+//
+// A NaN among a token's values of a KV head, K or V, makes the K exponent byte 255
+// (the others are 27 .. 227) and the K codes 0: 0 times infinity is NaN in the score,
+// so the rows that see the token are NaN.  V stays finite, so rows that do not see it
+// (weight 0) are not.
+//
+// Work per item: one workgroup for each (sequence, logical block) and KV head, as
+// in the append of the other pools; D / 8 lanes hold a row, 16 bytes each, and find
+// its maximum by shuffles.  V goes through LDS ([slot][d]) to the [d][slot] layout.
+// Bound by the launch and one round through memory for a decode step, by HBM for a
+// long suffix.
+#include <hip/hip_runtime.h>
+
+#include "internal.h"
+
+namespace pgsr {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256;
+constexpr int kExpLo = -100, kExpHi = 100;
+
+// What eight values of a row give: the largest magnitude's bits, and whether one is NaN.
+struct RowMax {
+  uint32_t bits = 0;      // of |x|, an integer order
+  bool nan = false;
+};
+
+__device__ inline void row_max(const uint16_t (&x)[8], RowMax& m) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t b = x[j] & 0x7FFFu;
+    if (b > 0x7F80u) m.nan = true;
+    else m.bits = max(m.bits, b);
+  }
+}
+
+// e of a row whose largest magnitude has these bf16 bits
+__device__ inline int row_exp(uint32_t bits) {
+  return min(max((int)(bits >> 7) - 127 - 6, kExpLo), kExpHi);   // zeros and subnormals: the lowest
+}
+
+// Eight codes of x 2^-e, in element order.
+__device__ inline u32x2 codes8(const uint16_t (&x)[8], int e, bool none) {
+  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+  u32x2 r = {0, 0};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float f = __uint_as_float((uint32_t)x[j] << 16) * inv;
+    const float c = fminf(fmaxf(__builtin_rintf(f), -127.f), 127.f);
+    const int code = none || f != f ? 0 : (int)c;
+    r[j / 4] |= (uint32_t)(uint8_t)code << (8 * (j % 4));
+  }
+  return r;
+}
+
+// Block ids, table, counts, lengths and stack top as append_kernel (kv_pool.hip)
+// writes them; the copies are the quantisation above.
+template <int B, int D>
+__global__ void __launch_bounds__(kThreads) append_int8_kernel(AppendArgs a) {
+  constexpr int C = D / 8;                         // lanes of a row
+  constexpr int RP = kThreads / C;                 // rows of a pass
+  constexpr int DP = D + 8;
+  __shared__ __attribute__((aligned(16))) uint8_t vstage[B * DP];
+  const int item = blockIdx.x, tid = threadIdx.x, h = blockIdx.y;
+  int ei = 0;
+  while (ei + 1 < a.n && a.e[ei + 1].item_start <= item) ++ei;
+  const AppendEntry e = a.e[ei];
+  const int32_t lb = e.lb_first + (item - e.item_start);
+  const int32_t p0 = max(e.prefix, lb * B);
+  const int32_t p1 = min(e.prefix + e.q_len, (lb + 1) * B);
+  int32_t* row = a.tables + (int64_t)e.seq * a.max_bps;
+  const int32_t cow_pops = e.cow_old >= 0 ? 1 : 0;   // cow_kernel took the first pop
+  const int32_t id = blk_id(lb < e.nalloc_before
+                                ? row[lb]
+                                : a.free_list[e.stack_before - 1 - cow_pops - (lb - e.nalloc_before)],
+                            a.n_blocks, a.chk);
+  if (h == 0 && tid == 0) {
+    if (lb >= e.nalloc_before) {
+      row[lb] = id;
+      a.refs[id] = 1;
+    }
+    if (a.commit && item == e.item_start) a.lens[e.seq] = e.prefix + e.q_len;
+    if (a.write_top && item == 0) *a.free_top = a.top_after;
+  }
+  const int64_t row_stride = (int64_t)a.n_kv_heads * D;
+  const int64_t src0 = ((int64_t)(e.q_off + (p0 - e.prefix)) * a.n_kv_heads + h) * D;
+  const int64_t blk = ((int64_t)a.layer * a.n_blocks + id) * a.n_kv_heads + h;
+  const uint16_t *kin = (const uint16_t*)a.k_in + src0, *vin = (const uint16_t*)a.v_in + src0;
+  uint8_t *kc = (uint8_t*)a.k_cache + blk * B * D, *vc = (uint8_t*)a.v_cache + blk * D * B;
+  uint8_t* ex = a.kv_exps + blk * 2 * B;
+  const int s0 = p0 - lb * B, nt = p1 - p0;
+  const bool wide = (((uintptr_t)kin | (uintptr_t)vin) & 15) == 0;
+
+  const int c = (tid % C) * 8;
+  for (int t0 = 0; t0 < nt; t0 += RP) {
+    const int t = t0 + tid / C;
+    uint16_t kx[8] = {}, vx[8] = {};
+    if (t < nt) {
+      const uint16_t *kp = kin + t * row_stride + c, *vp = vin + t * row_stride + c;
+      if (wide) {
+        const u32x4 kw = *(const u32x4*)kp, vw = *(const u32x4*)vp;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          kx[j] = (uint16_t)(kw[j / 2] >> (16 * (j % 2)));
+          vx[j] = (uint16_t)(vw[j / 2] >> (16 * (j % 2)));
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          kx[j] = kp[j];
+          vx[j] = vp[j];
+        }
+      }
+    }
+    RowMax mk, mv;
+    row_max(kx, mk);
+    row_max(vx, mv);
+    // both maxima and the flag through one word and one shuffle a step: magnitudes
+    // have 15 bits
+    uint32_t packed = mk.bits | (mv.bits << 16);
+    int nan = mk.nan || mv.nan;
+#pragma unroll
+    for (int off = C / 2; off >= 1; off >>= 1) {
+      const uint32_t o = __shfl_xor(packed, off);
+      packed = max(packed & 0xFFFFu, o & 0xFFFFu) | (max(packed >> 16, o >> 16) << 16);
+      nan |= __shfl_xor(nan, off);
+    }
+    if (t < nt) {
+      const int ke = row_exp(packed & 0xFFFFu), ve = row_exp(packed >> 16);
+      *(u32x2*)(kc + (s0 + t) * D + c) = codes8(kx, ke, nan != 0);
+      *(u32x2*)(&vstage[t * DP + c]) = codes8(vx, ve, false);
+      if (c == 0) {
+        ex[s0 + t] = nan ? 255 : (uint8_t)(ke + 127);
+        ex[B + s0 + t] = (uint8_t)(ve + 127);
+      }
+    }
+  }
+  __syncthreads();
+  if (s0 % 8 == 0 && nt % 8 == 0) {                // whole runs of 8 slots
+    const int runs = nt / 8;
+    for (int i = tid; i < D * runs; i += kThreads) {
+      const int d = i / runs, t0 = (i % runs) * 8;
+      u32x2 out = {0, 0};
+#pragma unroll
+      for (int x = 0; x < 8; ++x) out[x / 4] |= (uint32_t)vstage[(t0 + x) * DP + d] << (8 * (x % 4));
+      *(u32x2*)(vc + d * B + s0 + t0) = out;
+    }
+  } else {                                         // a partial first or last block: byte by byte
+    for (int i = tid; i < nt * D; i += kThreads) vc[(i % D) * B + s0 + i / D] = vstage[(i / D) * DP + i % D];
+  }
+}
+
+template <int B>
+void launch_b(const AppendArgs& a, hipStream_t s) {
+  const dim3 grid(a.n_items, a.n_kv_heads);
+  if (a.head_dim == 128) hipLaunchKernelGGL((append_int8_kernel<B, 128>), grid, dim3(kThreads), 0, s, a);
+  else hipLaunchKernelGGL((append_int8_kernel<B, 64>), grid, dim3(kThreads), 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_append_int8(const AppendArgs& a, hipStream_t s) {
+  if (a.n <= 0 || a.n_items <= 0) return hipSuccess;
+  if (!a.kv_exps || (a.head_dim != 64 && a.head_dim != 128)) return hipErrorInvalidValue;
+  const hipError_t err = launch_cow(a, 1, s);
+  if (err != hipSuccess) return err;
+  switch (a.block_size) {
+    case 16: launch_b<16>(a, s); break;
+    case 32: launch_b<32>(a, s); break;
+    case 64: launch_b<64>(a, s); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace pgsr

@@ -106,6 +106,10 @@ __global__ void __launch_bounds__(256) poison_kernel(PoisonArgs a, T nan) {
     const int32_t id = blk_id(a.free_list[a.top_before + blockIdx.x], a.n_blocks, a.chk);
     fill_nan(kc + (int64_t)id * blk_elems, blk_elems, nan, threadIdx.x, blockDim.x);
     fill_nan(vc + (int64_t)id * blk_elems, blk_elems, nan, threadIdx.x, blockDim.x);
+    if (a.kv_exps) {
+      const int64_t n = (int64_t)a.n_kv_heads * 2 * a.block_size;
+      fill_nan(a.kv_exps + ((int64_t)layer * a.n_blocks + id) * n, n, (uint8_t)0xFF, threadIdx.x, blockDim.x);
+    }
     return;
   }
   const CropEntry e = a.e[blockIdx.x - a.n_freed];
@@ -119,6 +123,8 @@ __global__ void __launch_bounds__(256) poison_kernel(PoisonArgs a, T nan) {
       const int slot = tail + r / D, c = r % D;
       kc[(int64_t)id * blk_elems + ((int64_t)h * B + slot) * D + c] = nan;
       vc[(int64_t)id * blk_elems + ((int64_t)h * D + c) * B + slot] = nan;
+      if (a.kv_exps && c < 2)
+        a.kv_exps[((((int64_t)layer * a.n_blocks + id) * a.n_kv_heads + h) * 2 + c) * B + slot] = 0xFF;
     }
   }
 }
@@ -153,6 +159,11 @@ __global__ void __launch_bounds__(256) cow_kernel(AppendArgs a) {
       const int c = i / s0, t = i % s0;
       vn[(int64_t)c * B + t] = vo[(int64_t)c * B + t];
     }
+    if (a.kv_exps)                                                          // [K, V][slot]
+      for (int i = threadIdx.x; i < 2 * s0; i += blockDim.x) {
+        const int at = (i / s0) * B + i % s0;
+        a.kv_exps[nb * 2 * B + at] = a.kv_exps[ob * 2 * B + at];
+      }
   }
 }
 
@@ -548,8 +559,9 @@ bool with_geometry(int block_size, int head_dim, F&& f) {
 }
 
 template <typename TI, typename T>
-hipError_t append_of(const AppendArgs& a, bool any_cow, hipStream_t s) {
-  if (any_cow) hipLaunchKernelGGL(cow_kernel<T>, dim3(a.n, a.n_kv_heads), dim3(256), 0, s, a);
+hipError_t append_of(const AppendArgs& a, hipStream_t s) {
+  const hipError_t err = launch_cow(a, sizeof(T), s);
+  if (err != hipSuccess) return err;
   const bool ok = with_geometry(a.block_size, a.head_dim, [&](auto b, auto d) {
     hipLaunchKernelGGL((append_kernel<TI, T, decltype(b)::value, decltype(d)::value>),
                        dim3(a.n_items, a.n_kv_heads), dim3(kAppendThreads<TI, T>), 0, s, a);
@@ -570,11 +582,20 @@ hipError_t fused_append_of(const FusedAppendArgs& a, hipStream_t s) {
 
 hipError_t launch_append(const AppendArgs& a, int elem_bytes, hipStream_t s) {
   if (a.n <= 0 || a.n_items <= 0) return hipSuccess;
+  return elem_bytes == 4   ? append_of<uint32_t, uint32_t>(a, s)
+         : elem_bytes == 2 ? append_of<uint16_t, uint16_t>(a, s)
+                           : append_of<uint16_t, uint8_t>(a, s);   // FP8 cache, bf16 inputs
+}
+
+hipError_t launch_cow(const AppendArgs& a, int elem_bytes, hipStream_t s) {
   bool any_cow = false;
   for (int i = 0; i < a.n; ++i) any_cow |= a.e[i].cow_old >= 0;
-  return elem_bytes == 4   ? append_of<uint32_t, uint32_t>(a, any_cow, s)
-         : elem_bytes == 2 ? append_of<uint16_t, uint16_t>(a, any_cow, s)
-                           : append_of<uint16_t, uint8_t>(a, any_cow, s);   // FP8 cache, bf16 inputs
+  if (!any_cow) return hipSuccess;
+  const dim3 grid(a.n, a.n_kv_heads);
+  if (elem_bytes == 4) hipLaunchKernelGGL(cow_kernel<uint32_t>, grid, dim3(256), 0, s, a);
+  else if (elem_bytes == 2) hipLaunchKernelGGL(cow_kernel<uint16_t>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cow_kernel<uint8_t>, grid, dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 bool fused_append_supported(int block_size, int head_dim) {

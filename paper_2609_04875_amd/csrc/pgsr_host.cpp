@@ -17,6 +17,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "attn_common.h"
 #include "internal.h"
 
 using namespace pgsr;
@@ -43,6 +44,8 @@ struct pgsr_pool {
   bool timing = false, timed_call = false;
   // FP8 pools: per-layer K and V scales (stored code = x / scale, read = code * scale)
   std::vector<float> k_scale, v_scale;
+  // int8 pools: exponent bytes (caller-owned; pgsr_pool_set_kv_exponents)
+  uint8_t* kv_exps = nullptr;
   // bf16 prefill kernel choice (PGSR_PREFILL_AUTO / _FOUR_WAVE / _PIPELINED)
   int prefill_kind = PGSR_PREFILL_AUTO;
   hipEvent_t ev[4] = {nullptr, nullptr, nullptr, nullptr};
@@ -106,6 +109,10 @@ int device_check(pgsr_pool* p, hipStream_t st) {
 inline int32_t cdiv(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
 
 int elem_bytes(const pgsr_pool* p) { return p->dtype == PGSR_F32 ? 4 : p->dtype == PGSR_BF16 ? 2 : 1; }
+
+int cache_kind(const pgsr_pool* p) {
+  return p->dtype == PGSR_FP8_E4M3 ? kCacheFp8 : p->dtype == PGSR_INT8 ? kCacheInt8 : kCacheBf16;
+}
 
 // Distinct, in-range sequence ids (a pairwise check for the few sequences of
 // a typical call, a table past that).
@@ -221,6 +228,7 @@ int do_crop(pgsr_pool* p, int32_t n, const int32_t* seqs, const int32_t* new_len
       pa.head_dim = p->d;
       pa.elem_bytes = elem_bytes(p);
       pa.top_before = a.top_before;
+      pa.kv_exps = p->kv_exps;
       pa.n_freed = p->h_top - a.top_before;
       pa.n = cnt;
       std::memcpy(pa.e, a.e, sizeof(CropEntry) * cnt);
@@ -321,6 +329,8 @@ int check_replay(const pgsr_pool* p, int32_t layer, int32_t n, const int32_t* se
   if (layer < 0 || layer >= p->n_layers)
     return fail(PGSR_EINVAL, "layer %d outside [0, %d)", layer, p->n_layers);
   if (!std::isfinite(scale)) return fail(PGSR_EINVAL, "softmax_scale is not finite");
+  if (p->dtype == PGSR_INT8 && !p->kv_exps)
+    return fail(PGSR_EINVAL, "the int8 pool has no exponents yet (pgsr_pool_set_kv_exponents)");
   int64_t total = 0, need = 0;
   // Private tail copies are decided in call order: each copy releases one
   // entry of the shared block, so the last row naming it writes in place.
@@ -494,7 +504,8 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
     a.n_items = items;
     a.write_top = 1;
     a.top_after = p->h_top;
-    hipError_t err = launch_append(a, eb, st);
+    a.kv_exps = p->kv_exps;
+    hipError_t err = p->dtype == PGSR_INT8 ? launch_append_int8(a, st) : launch_append(a, eb, st);
     if (err != hipSuccess) return hip_fail(err, "append launch");
   }
 
@@ -515,7 +526,8 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
   // plan is cut for the tiles of one of them: the four-wave kernel's where
   // PGSR_PREFILL_FOUR_WAVE asks for it, for FP8 and for groups that do not divide
   // 32, the larger ones of the others else.
-  const bool f8 = p->dtype == PGSR_FP8_E4M3;
+  const int cache = cache_kind(p);
+  const bool f8 = cache != kCacheBf16;             // one-byte codes: FP8 and int8
   const bool wide_ok = p->dtype == PGSR_BF16 && p->prefill_kind == PGSR_PREFILL_AUTO &&
                        attn_bf16_wide_eligible(p->d, group, p->B, p->n_blocks, p->hkv, max_kv);
   const bool pipe_ok = p->dtype != PGSR_F32 && p->prefill_kind != PGSR_PREFILL_FOUR_WAVE &&
@@ -548,6 +560,7 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
     a.layer = layer;
     a.scale_log2 = (float)((double)scale * 1.4426950408889634 * (double)p->k_scale[layer]);
     a.o_scale = p->v_scale[layer];
+    a.kv_exps = p->kv_exps;
     a.n = cnt;
     for (int32_t i = 0; i < cnt; ++i) {
       a.e[i].seq = chunk[i].seq;
@@ -593,7 +606,7 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
         a.e[i].tile_start = a.n_tiles;
         a.n_tiles += (a.n_splits > 1 ? cdiv(kv[i], a.split_len) : 1) * p->hkv;
       }
-      hipError_t err = launch_attn_decode(a, f8, st);
+      hipError_t err = launch_attn_decode(a, cache, st);
       if (err == hipSuccess && a.n_splits > 1) err = launch_split_combine(a, false, 16, st);
       if (err != hipSuccess) return hip_fail(err, "decode attention launch");
       continue;
@@ -684,8 +697,9 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
     hipError_t err = p->dtype == PGSR_F32 ? launch_attn_f32(a, st)
                      : narrow             ? launch_attn_bf16_narrow(a, narrow, st)
                      : wide               ? launch_attn_bf16_wide(a, st)
-                     : pipe               ? launch_attn_bf16_pipe(a, pipe, f8, st)
-                     : f8                 ? launch_attn_fp8(a, st)
+                     : pipe               ? launch_attn_bf16_pipe(a, pipe, cache, st)
+                     : cache == kCacheFp8  ? launch_attn_fp8(a, st)
+                     : cache == kCacheInt8 ? launch_attn_int8(a, st)
                                           : launch_attn_bf16(a, st);
     if (err == hipSuccess && a.n_splits > 1) err = launch_split_combine(a, p->dtype == PGSR_F32, p->dtype == PGSR_F32 ? 16 : 8, st);
     if (err != hipSuccess) return hip_fail(err, "attention launch");
@@ -739,7 +753,7 @@ int restore_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
   if (!crop_lens || n == 0)
     return do_replay(p, layer, n, seqs, q_lens, q, k, v, o, scale, flags, recomputed, p->workspace,
                      p->workspace_bytes, st);
-  bool fold = fused_append_supported(p->B, p->d) && n <= kMaxFusedSeqs;
+  bool fold = p->dtype != PGSR_INT8 && fused_append_supported(p->B, p->d) && n <= kMaxFusedSeqs;
   int64_t items = 0;
   for (int32_t i = 0; fold && i < n; ++i) {
     const int32_t L = crop_lens[i], S = q_lens[i];
@@ -803,7 +817,7 @@ int pgsr_pool_create(int32_t n_layers, int32_t n_q_heads, int32_t n_kv_heads, in
   if (n_q_heads % n_kv_heads != 0)
     return fail(PGSR_EUNSUPPORTED, "n_q_heads %d is not a multiple of n_kv_heads %d", n_q_heads,
                 n_kv_heads);
-  if (dtype != PGSR_F32 && dtype != PGSR_BF16 && dtype != PGSR_FP8_E4M3)
+  if (dtype != PGSR_F32 && dtype != PGSR_BF16 && dtype != PGSR_FP8_E4M3 && dtype != PGSR_INT8)
     return fail(PGSR_EUNSUPPORTED, "dtype %d", dtype);
   if (head_dim != 64 && head_dim != 128)
     return fail(PGSR_EUNSUPPORTED, "head_dim %d (supported: 64, 128)", head_dim);
@@ -811,7 +825,7 @@ int pgsr_pool_create(int32_t n_layers, int32_t n_q_heads, int32_t n_kv_heads, in
     return fail(PGSR_EUNSUPPORTED, "block_size %d (supported: 16, 32, 64)", block_size);
   const int group = n_q_heads / n_kv_heads;
   if (dtype != PGSR_F32 && group > 32)
-    return fail(PGSR_EUNSUPPORTED, "bf16 and fp8 kernels need n_q_heads / n_kv_heads <= 32");
+    return fail(PGSR_EUNSUPPORTED, "bf16, fp8 and int8 kernels need n_q_heads / n_kv_heads <= 32");
   if ((int64_t)max_seqs * max_blocks_per_seq > INT32_MAX)
     return fail(PGSR_ERANGE, "block table larger than 2^31-1 entries");
   if (!k_cache || !v_cache || !block_tables || !seq_lens || !free_list || !free_top || !ref_counts)
@@ -899,6 +913,14 @@ int pgsr_pool_set_kv_scales(pgsr_pool* p, const float* k_scales, const float* v_
         return fail(PGSR_EINVAL, "scale of layer %d is not a positive normal float", l);
   p->k_scale.assign(k_scales, k_scales + p->n_layers);
   p->v_scale.assign(v_scales, v_scales + p->n_layers);
+  return ok();
+}
+
+int pgsr_pool_set_kv_exponents(pgsr_pool* p, void* exponents) {
+  if (!p || !exponents) return fail(PGSR_EINVAL, "null argument");
+  if (p->dtype != PGSR_INT8) return fail(PGSR_EINVAL, "exponents apply to an int8 pool only");
+  if (((uintptr_t)exponents & 15) != 0) return fail(PGSR_EINVAL, "exponents must lie on a 16-byte boundary");
+  p->kv_exps = (uint8_t*)exponents;
   return ok();
 }
 

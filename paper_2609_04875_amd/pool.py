@@ -15,9 +15,9 @@ import torch
 from . import _native as N
 
 # (cache storage dtype, dtype of q / k / v / o) per pool dtype; an FP8 pool
-# holds raw E4M3 codes as bytes.
+# holds raw E4M3 codes as bytes, an int8 pool codes whose exponents lie apart.
 _DT = {N.F32: (torch.float32, torch.float32), N.BF16: (torch.bfloat16, torch.bfloat16),
-       N.FP8_E4M3: (torch.uint8, torch.bfloat16)}
+       N.FP8_E4M3: (torch.uint8, torch.bfloat16), N.INT8: (torch.int8, torch.bfloat16)}
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream], device: Optional[int] = None) -> Optional[int]:
@@ -88,6 +88,12 @@ class KVPool:
             workspace_bytes, order, _stream_ptr(stream), ctypes.byref(handle)))
         self._h = handle
         self._dev = self.k_cache.device.index
+        # int8 pools: the exponent byte (127 + e) of each token's K and V row, by KV head
+        self.kv_exponents = None
+        if dtype == N.INT8:
+            self.kv_exponents = torch.full((n_layers, n_blocks, n_kv_heads, 2, block_size), 27, dtype=torch.uint8,
+                                           device=device)
+            N.check(N.lib.pgsr_pool_set_kv_exponents(handle, self.kv_exponents.data_ptr()))
         self.recomputed_tokens = ctypes.c_int64(0)
 
     def close(self) -> None:
