@@ -374,6 +374,46 @@ int pgsr_gemm_silu_bf16(int32_t m, int32_t d_ff, int32_t k, const void *x, const
                         void *out, void *stream);
 
 /*
+ * The projections of F in 8-bit integers: half the weight bytes that a re-decoded
+ * token reads, and twice the matrix rate of bf16 for a long suffix.
+ *
+ * Rows of codes with a scale each: for a row y of k values
+ *   scales[r] = max |y_i| / 127,  q[r][i] = rint(y_i / scales[r])
+ * in fp32, ties to even; a row of zeros has scale 0, one that holds a NaN or an
+ * infinity (or whose mean square leaves fp32) scale NaN, both codes 0, so that its
+ * row of a product is NaN.  q [m][k] int8, scales fp32 [m].
+ *   pgsr_quantize_rows_int8: y = x [m][k], dtype PGSR_BF16 or PGSR_F32: the states
+ *     of m tokens, or a weight [n][k] for a scale to each output channel;
+ *   pgsr_rmsnorm_int8: y = x / sqrt(mean(x^2) + eps) * gain, not rounded in
+ *     between (x, gain bf16);
+ *   pgsr_silu_mul_int8: y = SiLU(gate) * up of bf16 gate_up [m][2 d_ff], k = d_ff.
+ * k a multiple of 16, at most 133136 (PGSR_EUNSUPPORTED else); x, gain, gate_up
+ * and q on 16-byte boundaries (PGSR_EINVAL else).
+ */
+int pgsr_quantize_rows_int8(int32_t m, int32_t k, int32_t dtype, const void *x, void *q, float *scales,
+                            void *stream);
+int pgsr_rmsnorm_int8(int32_t m, int32_t k, const void *x, const void *gain, float eps, void *q,
+                      float *scales, void *stream);
+int pgsr_silu_mul_int8(int32_t m, int32_t d_ff, const void *gate_up, void *q, float *scales, void *stream);
+
+/*
+ * Y[m][n] = (sum_k x[m][k] w[n][k]) * (xs[m] * ws[n]) (+ R[m][n] when R != NULL):
+ * int8 codes x [m][k] and w [n][k], a fp32 scale for each token and each output
+ * channel, bf16 R and Y (R may alias Y).  The sum is exact (int32); product with
+ * the scales and the addition in fp32, one round-to-nearest-even store; rows do not
+ * depend on the others.  Codes are -127 .. 127; -128 is summed exactly as well for
+ * k up to 131056.  n a multiple of 8, k of 16 up to 133136 (PGSR_EUNSUPPORTED else);
+ * x, w and ws on 16-byte boundaries, R and Y on 8-byte ones (PGSR_EINVAL else);
+ * m * n, in whole tiles, below 2^34 (PGSR_ERANGE else).  The second form: up to
+ * three weights that share x, in one launch, the same bits.
+ */
+int pgsr_gemm_int8(int32_t m, int32_t n, int32_t k, const void *x, const float *xs, const void *w,
+                   const float *ws, const void *r, void *y, void *stream);
+int pgsr_gemm_int8_multi(int32_t m, int32_t k, int32_t count, const int32_t *n, const void *x,
+                         const float *xs, const void *const *w, const float *const *ws, void *const *y,
+                         void *stream);
+
+/*
  * Elementwise steps of a full decoder layer around the projections (F of
  * Eq. (1) at the real geometries; the layer itself follows the public
  * architecture of the model families the paper runs).  bf16 device arrays,

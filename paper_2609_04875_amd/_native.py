@@ -34,7 +34,8 @@ EXPORTS = (
     "pgsr_ckpt_destroy", "pgsr_ckpt_register", "pgsr_ckpt_count", "pgsr_forget_plan_query",
     "pgsr_sample_workspace_bytes", "pgsr_sample_tokens", "pgsr_rmsnorm_bf16", "pgsr_rope_bf16",
     "pgsr_rope_qk_bf16",
-    "pgsr_silu_mul_bf16",
+    "pgsr_silu_mul_bf16", "pgsr_quantize_rows_int8", "pgsr_rmsnorm_int8", "pgsr_silu_mul_int8",
+    "pgsr_gemm_int8", "pgsr_gemm_int8_multi",
 )
 
 
@@ -129,6 +130,15 @@ def _load() -> ctypes.CDLL:
     lib.pgsr_rope_qk_bf16.argtypes = [i32, i32, i32, i32, P, P, P, ctypes.c_double, P]
     lib.pgsr_silu_mul_bf16.restype = ctypes.c_int
     lib.pgsr_silu_mul_bf16.argtypes = [i32, i32, P, P, P]
+    for name, args in (
+            ("pgsr_quantize_rows_int8", [i32, i32, i32, P, P, P, P]),
+            ("pgsr_rmsnorm_int8", [i32, i32, P, P, f32, P, P, P]),
+            ("pgsr_silu_mul_int8", [i32, i32, P, P, P, P]),
+            ("pgsr_gemm_int8", [i32, i32, i32, P, P, P, P, P, P, P]),
+            ("pgsr_gemm_int8_multi", [i32, i32, i32, P, P, P, P, P, P, P])):
+        f = getattr(lib, name)
+        f.restype = ctypes.c_int
+        f.argtypes = args
     # forget front-end (host only)
     i64p = ctypes.POINTER(i64)
     for name, args in (

@@ -326,4 +326,16 @@ bool gemm_bf16_wide_eligible(int m, int n, int k);
 hipError_t launch_gemm_bf16_wide(int m, int n, int k, const void* x, const void* w, const void* r,
                                  void* y, hipStream_t s);
 
+// Int8 rows with a scale each (k a multiple of 16): of bf16 or fp32 rows, behind
+// RMSNorm, and of the SwiGLU product of gate_up [m][2 k].
+hipError_t launch_quantize_rows(int32_t m, int32_t k, bool f32, const void* x, void* q, float* scales, hipStream_t s);
+hipError_t launch_rmsnorm_int8(int32_t m, int32_t k, const void* x, const void* gain, float eps, void* q, float* scales,
+                               hipStream_t s);
+hipError_t launch_silu_mul_int8(int32_t m, int32_t k, const void* gate_up, void* q, float* scales, hipStream_t s);
+// Whether a product fits one launch.
+bool gemm_int8_fits(int m, int count, const int* n);
+// Up to kGemmMulti int8 products of the same x, in one launch (r: of the first alone).
+hipError_t launch_gemm_int8(int m, int k, int count, const int* n, const void* x, const float* xs,
+                            const void* const* w, const float* const* ws, const void* r, void* const* y, hipStream_t s);
+
 }  // namespace pgsr

@@ -1241,6 +1241,76 @@ int pgsr_gemm_silu_bf16(int32_t m, int32_t d_ff, int32_t k, const void* x, const
   return err == hipSuccess ? ok() : hip_fail(err, "gemm + silu launch");
 }
 
+// ---------------------------------------------------------- int8 products -- //
+// k: rows of codes end on 16-byte boundaries; past kInt8MaxK a sum of 127 * 127 could
+// leave int32.
+constexpr int32_t kInt8MaxK = 133136;
+
+static int check_int8_rows(const char* what, int32_t m, int32_t k, const void* x, const void* q, const void* scales) {
+  if (m < 0 || k <= 0) return fail(PGSR_EINVAL, "%s: m = %d, k = %d", what, m, k);
+  if (k % 16 || k > kInt8MaxK) return fail(PGSR_EUNSUPPORTED, "%s: k = %d (multiples of 16 up to %d)", what, k, kInt8MaxK);
+  if (m == 0) return PGSR_OK;
+  if (!x || !q || !scales) return fail(PGSR_EINVAL, "%s: null pointer", what);
+  if (!aligned16(x) || !aligned16(q) || ((uintptr_t)scales & 3))
+    return fail(PGSR_EINVAL, "%s: x and codes must lie on 16-byte boundaries, scales on their own", what);
+  return PGSR_OK;
+}
+
+int pgsr_quantize_rows_int8(int32_t m, int32_t k, int32_t dtype, const void* x, void* q, float* scales, void* stream) {
+  if (dtype != PGSR_F32 && dtype != PGSR_BF16) return fail(PGSR_EUNSUPPORTED, "dtype %d", dtype);
+  const int rc = check_int8_rows("quantize_rows", m, k, x, q, scales);
+  if (rc) return rc;
+  hipError_t err = launch_quantize_rows(m, k, dtype == PGSR_F32, x, q, scales, (hipStream_t)stream);
+  return err == hipSuccess ? ok() : hip_fail(err, "quantize_rows launch");
+}
+
+int pgsr_rmsnorm_int8(int32_t m, int32_t k, const void* x, const void* gain, float eps, void* q, float* scales,
+                      void* stream) {
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(PGSR_EINVAL, "eps must be finite and >= 0");
+  const int rc = check_int8_rows("rmsnorm_int8", m, k, x, q, scales);
+  if (rc) return rc;
+  if (m > 0 && (!gain || !aligned16(gain))) return fail(PGSR_EINVAL, "rmsnorm_int8: gain must lie on a 16-byte boundary");
+  hipError_t err = launch_rmsnorm_int8(m, k, x, gain, eps, q, scales, (hipStream_t)stream);
+  return err == hipSuccess ? ok() : hip_fail(err, "rmsnorm_int8 launch");
+}
+
+int pgsr_silu_mul_int8(int32_t m, int32_t d_ff, const void* gate_up, void* q, float* scales, void* stream) {
+  const int rc = check_int8_rows("silu_mul_int8", m, d_ff, gate_up, q, scales);
+  if (rc) return rc;
+  hipError_t err = launch_silu_mul_int8(m, d_ff, gate_up, q, scales, (hipStream_t)stream);
+  return err == hipSuccess ? ok() : hip_fail(err, "silu_mul_int8 launch");
+}
+
+// Products of one X: the checks of both entry points, then the launch.
+static int gemm_int8(int32_t m, int32_t k, int32_t count, const int32_t* n, const void* x, const float* xs,
+                     const void* const* w, const float* const* ws, const void* r, void* const* y, void* stream) {
+  if (m < 0 || k <= 0) return fail(PGSR_EINVAL, "gemm_int8: m = %d, k = %d", m, k);
+  if (k % 16 || k > kInt8MaxK) return fail(PGSR_EUNSUPPORTED, "gemm_int8: k = %d (multiples of 16 up to %d)", k, kInt8MaxK);
+  for (int32_t i = 0; i < count; ++i) {
+    if (n[i] < 0) return fail(PGSR_EINVAL, "gemm_int8: n = %d", n[i]);
+    if (n[i] % 8) return fail(PGSR_EUNSUPPORTED, "gemm_int8: n = %d (multiples of 8)", n[i]);
+    if (m == 0 || n[i] == 0) continue;
+    if (!x || !xs || !w[i] || !ws[i] || !y[i]) return fail(PGSR_EINVAL, "gemm_int8: null pointer");
+    if (!aligned16(x) || !aligned16(w[i]) || !aligned16(ws[i]) || ((uintptr_t)xs & 3) || (((uintptr_t)y[i] | (uintptr_t)r) & 7))
+      return fail(PGSR_EINVAL, "gemm_int8: codes and channel scales must lie on 16-byte boundaries, y and r on 8-byte ones");
+  }
+  if (!gemm_int8_fits(m, count, n)) return fail(PGSR_ERANGE, "gemm_int8: m = %d: too many tiles for one launch", m);
+  hipError_t err = launch_gemm_int8(m, k, count, n, x, xs, w, ws, r, y, (hipStream_t)stream);
+  return err == hipSuccess ? ok() : hip_fail(err, "gemm_int8 launch");
+}
+
+int pgsr_gemm_int8(int32_t m, int32_t n, int32_t k, const void* x, const float* xs, const void* w, const float* ws,
+                   const void* r, void* y, void* stream) {
+  return gemm_int8(m, k, 1, &n, x, xs, &w, &ws, r, &y, stream);
+}
+
+int pgsr_gemm_int8_multi(int32_t m, int32_t k, int32_t count, const int32_t* n, const void* x, const float* xs,
+                         const void* const* w, const float* const* ws, void* const* y, void* stream) {
+  if (count < 1 || count > kGemmMulti) return fail(PGSR_EINVAL, "count = %d (1 to %d)", count, kGemmMulti);
+  if (!n || !w || !ws || !y) return fail(PGSR_EINVAL, "null array");
+  return gemm_int8(m, k, count, n, x, xs, w, ws, nullptr, y, stream);
+}
+
 // Vocabulary entries per sampling workgroup (a multiple of 4: Philox blocks
 // never straddle two chunks).
 constexpr int32_t kSampleChunk = 8192;

@@ -1,0 +1,201 @@
+// Rows of int8 codes with a scale for each: the left operand of the int8 product
+// (a token's states, behind RMSNorm or the SwiGLU product where they are quantised
+// next) and, from a weight in the [out][in] layout, its codes with a scale for each
+// output channel.
+//
+// For a row y of k fp32 values: s = max |y_i| / 127, code_i = rint(y_i / s) (fp32
+// divisions, ties to even), so |code_i s - y_i| <= s / 2; a row of zeros has s = 0 and
+// codes 0; one that holds a NaN or an infinity has s = NaN and codes 0, which makes
+// its row of the product NaN.  y is x itself (bf16 or fp32), x / sqrt(mean(x^2) + eps)
+// * gain, or SiLU(gate) * up, in fp32 and not rounded in between.  Magnitudes are
+// compared as integers (of the bits without the sign), where NaN is the largest.
+//
+// One workgroup a row, the whole row in registers: a row is read once and its codes
+// written once, which bounds it (HBM for many rows, one pass through memory and two
+// reductions for a few).  256 threads; 1024 where the rows leave CUs idle, so that one
+// row is in flight at once.
+#include <hip/hip_runtime.h>
+
+#include "elementwise.h"
+#include "internal.h"
+
+namespace pgsr {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+enum Front { kRowsBf16, kRowsF32, kNorm, kGate };
+
+// Eight values of a row from column c; NORM: x * gain, still without the factor of
+// the row, and their squares' sum.
+template <int F>
+__device__ inline void load8(const void* x, const uint16_t* gain, int64_t row, int32_t k, int c, float (&y)[8],
+                             float& ss) {
+  if constexpr (F == kRowsF32) {
+    const float* p = (const float*)x + row * k + c;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 v = *(const f32x4*)(p + 4 * h);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[4 * h + j] = v[j];
+    }
+  } else if constexpr (F == kGate) {
+    const uint16_t* p = (const uint16_t*)x + row * 2 * k + c;
+    const u32x4 g = *(const u32x4*)p, u = *(const u32x4*)(p + k);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      y[2 * j] = silu_f32(lo_bf16(g[j])) * lo_bf16(u[j]);
+      y[2 * j + 1] = silu_f32(hi_bf16(g[j])) * hi_bf16(u[j]);
+    }
+  } else {
+    const u32x4 v = *(const u32x4*)((const uint16_t*)x + row * k + c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      y[2 * j] = lo_bf16(v[j]);
+      y[2 * j + 1] = hi_bf16(v[j]);
+    }
+    if constexpr (F == kNorm) {
+      const u32x4 w = *(const u32x4*)(gain + c);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        ss = fmaf(y[2 * j], y[2 * j], ss);
+        ss = fmaf(y[2 * j + 1], y[2 * j + 1], ss);
+        y[2 * j] *= lo_bf16(w[j]);
+        y[2 * j + 1] *= hi_bf16(w[j]);
+      }
+    }
+  }
+}
+
+__device__ inline uint32_t mag8(const float (&y)[8], uint32_t m) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(y[j]) & 0x7FFFFFFFu);
+  return m;
+}
+
+// codes of y * f / s (f: the factor of a normalised row, else 1)
+__device__ inline u32x2 codes8(const float (&y)[8], float f, float s, bool none) {
+  u32x2 r = {0, 0};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float q = __builtin_rintf(y[j] * f / s);
+    const int code = none ? 0 : (int)fminf(fmaxf(q, -127.f), 127.f);   // past it by subnormal scales only
+    r[j / 4] |= (uint32_t)(uint8_t)code << (8 * (j % 4));
+  }
+  return r;
+}
+
+// NC chunks of 8 a thread hold the row; NC = 0: a longer row, read twice.
+template <int F, int NT, int NC>
+__global__ void __launch_bounds__(NT) quantize_kernel(int32_t k, const void* __restrict__ x,
+                                                      const uint16_t* __restrict__ gain, float eps,
+                                                      uint8_t* __restrict__ q, float* __restrict__ scales) {
+  __shared__ uint32_t red_m[NT / 64];
+  __shared__ float red_s[NT / 64];
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x, chunks = k / 8;
+  float y[NC > 0 ? NC : 1][8];
+  float ss = 0.f;
+  uint32_t m = 0;
+  if constexpr (NC > 0) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      if (tid + i * NT < chunks) load8<F>(x, gain, row, k, (tid + i * NT) * 8, y[i], ss);
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      if (tid + i * NT < chunks) m = mag8(y[i], m);
+  } else {
+    for (int c = tid; c < chunks; c += NT) {
+      load8<F>(x, gain, row, k, c * 8, y[0], ss);
+      m = mag8(y[0], m);
+    }
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    m = max(m, (uint32_t)__shfl_xor((int)m, off));
+    if constexpr (F == kNorm) ss += __shfl_xor(ss, off);
+  }
+  if ((tid & 63) == 0) {
+    red_m[tid >> 6] = m;
+    if constexpr (F == kNorm) red_s[tid >> 6] = ss;
+  }
+  __syncthreads();
+  m = 0;
+  ss = 0.f;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    m = max(m, red_m[w]);
+    if constexpr (F == kNorm) ss += red_s[w];
+  }
+  float f = 1.f, top = __uint_as_float(m);
+  if constexpr (F == kNorm) {
+    f = 1.f / sqrtf(ss / (float)k + eps);
+    top *= f;
+  }
+  // a NaN or an infinity in the row; behind the norm also a row whose mean square is
+  // 0 with eps 0 or leaves fp32
+  const bool bad = !(top < INFINITY) || (F == kNorm && !(ss < INFINITY && f < INFINITY));
+  const float s = bad ? __uint_as_float(0x7FC00000u) : top / 127.f;
+  const bool none = bad || s == 0.f;
+  if (tid == 0) scales[row] = s;
+  uint8_t* out = q + row * k;
+  if constexpr (NC > 0) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      if (tid + i * NT < chunks) *(u32x2*)(out + (tid + i * NT) * 8) = codes8(y[i], f, s, none);
+  } else {
+    for (int c = tid; c < chunks; c += NT) {
+      load8<F>(x, gain, row, k, c * 8, y[0], ss);
+      *(u32x2*)(out + c * 8) = codes8(y[0], f, s, none);
+    }
+  }
+}
+
+template <int F, int NT>
+void launch_nt(int32_t m, int32_t k, const void* x, const void* gain, float eps, void* q, float* scales, hipStream_t st) {
+  const int per = (k / 8 + NT - 1) / NT;
+  auto go = [&](auto nc) {
+    constexpr int32_t kRows = 1 << 21;             // a launch counts its threads in 32 bits
+    for (int32_t r0 = 0; r0 < m; r0 += kRows) {
+      const int64_t at = (int64_t)r0 * k * (F == kRowsF32 || F == kGate ? 4 : 2);
+      hipLaunchKernelGGL((quantize_kernel<F, NT, decltype(nc)::value>), dim3(min(kRows, m - r0)), dim3(NT), 0, st, k,
+                         (const char*)x + at, (const uint16_t*)gain, eps, (uint8_t*)q + (int64_t)r0 * k, scales + r0);
+      if (m - r0 <= kRows) break;
+    }
+  };
+  if (per <= 1) go(std::integral_constant<int, 1>{});
+  else if (per <= 2) go(std::integral_constant<int, 2>{});
+  else if (per <= 4) go(std::integral_constant<int, 4>{});
+  else if (per <= 8 && NT == 256) go(std::integral_constant<int, NT == 256 ? 8 : 0>{});
+  else go(std::integral_constant<int, 0>{});
+}
+
+template <int F>
+hipError_t launch_front(int32_t m, int32_t k, const void* x, const void* gain, float eps, void* q, float* scales,
+                        hipStream_t st) {
+  if (m <= 0) return hipSuccess;
+  if (k > 256 * 8 && (m <= 256 || k > 256 * 8 * 8)) launch_nt<F, 1024>(m, k, x, gain, eps, q, scales, st);
+  else launch_nt<F, 256>(m, k, x, gain, eps, q, scales, st);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize_rows(int32_t m, int32_t k, bool f32, const void* x, void* q, float* scales, hipStream_t s) {
+  return f32 ? launch_front<kRowsF32>(m, k, x, nullptr, 0.f, q, scales, s)
+             : launch_front<kRowsBf16>(m, k, x, nullptr, 0.f, q, scales, s);
+}
+
+hipError_t launch_rmsnorm_int8(int32_t m, int32_t k, const void* x, const void* gain, float eps, void* q, float* scales,
+                               hipStream_t s) {
+  return launch_front<kNorm>(m, k, x, gain, eps, q, scales, s);
+}
+
+hipError_t launch_silu_mul_int8(int32_t m, int32_t k, const void* gate_up, void* q, float* scales, hipStream_t s) {
+  return launch_front<kGate>(m, k, gate_up, nullptr, 0.f, q, scales, s);
+}
+
+}  // namespace pgsr

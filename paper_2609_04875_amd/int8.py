@@ -1,0 +1,119 @@
+"""8-bit integer projections (``pgsr_gemm_int8`` and what makes its operands, in
+``include/pgsr.h``): codes with a scale for each token and each output channel.
+Marshalling only.
+
+A weight is quantised once, ``wq, ws = quantize_rows(w)`` ([out, in]: a scale for
+each output channel); a call quantises its tokens (``quantize_rows``,
+``rmsnorm_int8``, ``silu_mul_int8``) and multiplies (``gemm_int8``).
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Sequence, Tuple
+
+import torch
+
+from . import _native as N
+from .pool import _dev_ptr, _stream_ptr
+
+_DT = {torch.float32: N.F32, torch.bfloat16: N.BF16}
+Rows = Tuple[torch.Tensor, torch.Tensor]
+
+
+def _device(x: torch.Tensor, name: str) -> int:
+    """Index of the device ``x`` is on, which must be the current one: kernels are
+    launched there."""
+    dv = x.device.index
+    if not x.is_cuda or dv != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {x.device}; the current device is cuda:{torch.cuda.current_device()}")
+    return dv
+
+
+def _rows(m: int, k: int, dv: int, out: Optional[torch.Tensor], scales: Optional[torch.Tensor]):
+    """Codes [m, k] and scales [m] of a call, given or new, and their addresses."""
+    if out is None:
+        out = torch.empty((m, k), dtype=torch.int8, device=torch.device("cuda", dv))
+    if scales is None:
+        scales = torch.empty((m,), dtype=torch.float32, device=torch.device("cuda", dv))
+    return (out, scales), (_dev_ptr(out, torch.int8, "out", dv, m * k),
+                           _dev_ptr(scales, torch.float32, "scales", dv, m))
+
+
+def quantize_rows(x: torch.Tensor, out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                  stream=None) -> Rows:
+    """Codes (int8 [m, k]) and scales (fp32 [m]) of the rows of ``x`` [m, k], bf16
+    or fp32: scale = max |x| / 127, code = rint(x / scale)."""
+    if x.dim() != 2 or x.dtype not in _DT:
+        raise ValueError(f"x is {tuple(x.shape)} {x.dtype}; it must be [m, k], bf16 or fp32")
+    (m, k), dv = x.shape, _device(x, "x")
+    rows, at = _rows(m, k, dv, out, scales)
+    N.check(N.lib.pgsr_quantize_rows_int8(m, k, _DT[x.dtype], _dev_ptr(x, x.dtype, "x", dv), *at, _stream_ptr(stream, dv)))
+    return rows
+
+
+def rmsnorm_int8(x: torch.Tensor, gain: torch.Tensor, eps: float, out: Optional[torch.Tensor] = None,
+                 scales: Optional[torch.Tensor] = None, stream=None) -> Rows:
+    """``quantize_rows`` of x / sqrt(mean(x^2) + eps) * gain (bf16 ``x`` [m, k],
+    ``gain`` [k]), with no rounding in between."""
+    if x.dim() != 2:
+        raise ValueError(f"x is {tuple(x.shape)}; it must be [m, k]")
+    (m, k), dv = x.shape, _device(x, "x")
+    rows, at = _rows(m, k, dv, out, scales)
+    N.check(N.lib.pgsr_rmsnorm_int8(m, k, _dev_ptr(x, torch.bfloat16, "x", dv),
+                                    _dev_ptr(gain, torch.bfloat16, "gain", dv, k), float(eps), *at,
+                                    _stream_ptr(stream, dv)))
+    return rows
+
+
+def silu_mul_int8(gate_up: torch.Tensor, out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                  stream=None) -> Rows:
+    """``quantize_rows`` of SiLU(gate) * up for bf16 ``gate_up`` [m, 2 d_ff] (gate,
+    then up), with no rounding in between."""
+    if gate_up.dim() != 2 or gate_up.shape[1] % 2:
+        raise ValueError(f"gate_up is {tuple(gate_up.shape)}; it must be [m, 2 d_ff]")
+    (m, k), dv = (gate_up.shape[0], gate_up.shape[1] // 2), _device(gate_up, "gate_up")
+    rows, at = _rows(m, k, dv, out, scales)
+    N.check(N.lib.pgsr_silu_mul_int8(m, k, _dev_ptr(gate_up, torch.bfloat16, "gate_up", dv), *at, _stream_ptr(stream, dv)))
+    return rows
+
+
+def _weight(wq: torch.Tensor, ws: torch.Tensor, k: int, dv: int):
+    if wq.dim() != 2 or wq.shape[1] != k:
+        raise ValueError(f"w is {tuple(wq.shape)}; x has k = {k}")
+    return _dev_ptr(wq, torch.int8, "w", dv), _dev_ptr(ws, torch.float32, "ws", dv, wq.shape[0])
+
+
+def gemm_int8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, r: Optional[torch.Tensor] = None,
+              out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Y = (Xq Wq^T) * xs * ws (+ R), bf16: int8 codes ``xq`` [m, k], ``wq`` [n, k],
+    fp32 scales of the tokens ``xs`` [m] and of the output channels ``ws`` [n]; the
+    sums are exact.  ``r`` may be ``out``."""
+    if xq.dim() != 2:
+        raise ValueError(f"x is {tuple(xq.shape)}; it must be [m, k]")
+    (m, k), dv, bf = xq.shape, _device(xq, "x"), torch.bfloat16
+    wp, wsp = _weight(wq, ws, k, dv)
+    n = wq.shape[0]
+    if out is None:
+        out = torch.empty((m, n), dtype=bf, device=xq.device)
+    N.check(N.lib.pgsr_gemm_int8(m, n, k, _dev_ptr(xq, torch.int8, "x", dv), _dev_ptr(xs, torch.float32, "xs", dv, m), wp, wsp,
+                                 _dev_ptr(r, bf, "r", dv, m * n) if r is not None else None,
+                                 _dev_ptr(out, bf, "out", dv, m * n), _stream_ptr(stream, dv)))
+    return out
+
+
+def gemm_int8_multi(xq: torch.Tensor, xs: torch.Tensor, wqs: Sequence[torch.Tensor], wss: Sequence[torch.Tensor],
+                    outs: Sequence[torch.Tensor], stream=None) -> Sequence[torch.Tensor]:
+    """out_i = (Xq Wq_i^T) * xs * ws_i for up to three weights: the bits of one
+    ``gemm_int8`` each, in one launch."""
+    if xq.dim() != 2:
+        raise ValueError(f"x is {tuple(xq.shape)}; it must be [m, k]")
+    (m, k), dv, c = xq.shape, _device(xq, "x"), len(wqs)
+    if len(wss) != c or len(outs) != c:
+        raise ValueError(f"{c} weights but {len(wss)} scales and {len(outs)} outputs")
+    at = [_weight(wq, ws, k, dv) for wq, ws in zip(wqs, wss)]
+    ns = (ctypes.c_int32 * c)(*(w.shape[0] for w in wqs))
+    yp = (ctypes.c_void_p * c)(*(_dev_ptr(o, torch.bfloat16, "out", dv, m * n) for o, n in zip(outs, ns)))
+    N.check(N.lib.pgsr_gemm_int8_multi(m, k, c, ns, _dev_ptr(xq, torch.int8, "x", dv),
+                                       _dev_ptr(xs, torch.float32, "xs", dv, m), (ctypes.c_void_p * c)(*(p for p, _ in at)),
+                                       (ctypes.c_void_p * c)(*(p for _, p in at)), yp, _stream_ptr(stream, dv)))
+    return outs
