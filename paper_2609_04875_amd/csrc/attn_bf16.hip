@@ -402,14 +402,21 @@ __global__ void __launch_bounds__(256) split_combine_kernel(AttnArgs a, TO* __re
   constexpr int TPR = D / 8;                       // threads per row
   const int64_t row = a.row_begin + (int64_t)blockIdx.x * (blockDim.x / TPR) + threadIdx.x / TPR;
   const int c0 = (threadIdx.x % TPR) * 8;
-  if (row >= a.row_end) return;
   const int tok = (int)(row / a.n_q_heads);        // packed query token
-  int ei = -1;                                     // entries are not sorted by q_off
-  for (int i = 0; i < a.n; ++i)
-    if (tok >= a.e[i].q_off && tok < a.e[i].q_off + a.e[i].q_len) ei = i;
-  if (ei < 0) return;                              // a row of no entry of this launch
-  const AttnEntry e = a.e[ei];
-  const int qpos = e.prefix + (tok - e.q_off);
+  // Entries are not sorted by q_off: lane i holds entry i, and each of the wave's rows
+  // asks all of them (walking them costs a round through memory each: 32 sequences 8.2
+  // us a launch).
+  const int lane = threadIdx.x & 63;
+  const AttnEntry mine = a.e[min(lane, a.n - 1)];
+  int qpos = -1;
+#pragma unroll
+  for (int r = 0; r < 64 / TPR; ++r) {
+    const int t = __builtin_amdgcn_readlane(tok, r * TPR);
+    const uint64_t in = __ballot(lane < a.n && t >= mine.q_off && t < mine.q_off + mine.q_len);
+    const int pos = in ? __builtin_amdgcn_readlane(mine.prefix + t - mine.q_off, __builtin_ctzll(in)) : -1;
+    if (lane / TPR == r) qpos = pos;
+  }
+  if (row >= a.row_end || qpos < 0) return;        // a row of no entry of this launch
   const int ns = min(a.n_splits, qpos / a.split_len + 1);
   const float* __restrict__ ml = a.ws_ml;
   const float* __restrict__ acc = a.ws_acc;
