@@ -29,6 +29,17 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 enum Front { kRowsBf16, kRowsF32, kNorm, kGate };
 
+// SiLU(g) = g / (1 + e^-g) to about three roundings: e^-g = 2^t (1 + rest ln 2) with
+// t = -g log2(e) rounded and the rest kept, so a large |g| loses nothing; t past 126 is
+// cut (the result is below 2^-100 there).
+__device__ inline float silu_fast(float g) {
+  constexpr float kL = 1.44269504f, kLLo = 1.92596299e-8f;   // log2(e) = kL + kLLo
+  const float t = fminf(g * -kL, 126.f);
+  const float rest = fmaf(g, -kLLo, fmaf(g, -kL, -t));
+  const float e = __builtin_amdgcn_exp2f(t);
+  return g * __builtin_amdgcn_rcpf(1.f + fmaf(e, t < 126.f ? rest * 0.69314718f : 0.f, e));
+}
+
 // Eight values of a row from column c; NORM: x * gain, still without the factor of
 // the row, and their squares' sum.
 template <int F>
@@ -47,8 +58,8 @@ __device__ inline void load8(const void* x, const uint16_t* gain, int64_t row, i
     const u32x4 g = *(const u32x4*)p, u = *(const u32x4*)(p + k);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      y[2 * j] = silu_f32(lo_bf16(g[j])) * lo_bf16(u[j]);
-      y[2 * j + 1] = silu_f32(hi_bf16(g[j])) * hi_bf16(u[j]);
+      y[2 * j] = silu_fast(lo_bf16(g[j])) * lo_bf16(u[j]);
+      y[2 * j + 1] = silu_fast(hi_bf16(g[j])) * hi_bf16(u[j]);
     }
   } else {
     const u32x4 v = *(const u32x4*)((const uint16_t*)x + row * k + c);
@@ -76,16 +87,33 @@ __device__ inline uint32_t mag8(const float (&y)[8], uint32_t m) {
   return m;
 }
 
-// codes of y * f / s (f: the factor of a normalised row, else 1)
-__device__ inline u32x2 codes8(const float (&y)[8], float f, float s, bool none) {
-  u32x2 r = {0, 0};
+// Codes of y / s, r = 1 / s.  EXACT: the quotient rounded as a division rounds it, in
+// three instructions instead of ten (the remainder y - q s of q = y r is exact in one
+// fused operation, and its part of r corrects q), which a value of the input that lies
+// half way between two codes needs.  Behind the norm and the gate y itself is off by
+// some roundings, and q alone moves a code once in 10^5.
+template <bool EXACT>
+__device__ inline u32x2 codes8(const float (&y)[8], float s, float r) {
+  u32x2 out = {0, 0};
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float q = __builtin_rintf(y[j] * f / s);
-    const int code = none ? 0 : (int)fminf(fmaxf(q, -127.f), 127.f);   // past it by subnormal scales only
-    r[j / 4] |= (uint32_t)(uint8_t)code << (8 * (j % 4));
+    float q = y[j] * r;
+    if constexpr (EXACT) q = fmaf(fmaf(-q, s, y[j]), r, q);
+    // |q| <= 127 and a rounding: rint(q) is in the low byte of q + 3 * 2^22
+    const uint32_t b = __float_as_uint(q + 12582912.f);
+    out[j / 4] |= (b & 0xFFu) << (8 * (j % 4));
   }
-  return r;
+  return out;
+}
+// Scales so small (or large) that 1 / s or the remainder leaves fp32's normal range.
+__device__ inline u32x2 codes8_far(const float (&y)[8], float s) {
+  u32x2 out = {0, 0};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int code = (int)fminf(fmaxf(__builtin_rintf(y[j] / s), -127.f), 127.f);   // past 127 by subnormal scales only
+    out[j / 4] |= (uint32_t)(uint8_t)code << (8 * (j % 4));
+  }
+  return out;
 }
 
 // NC chunks of 8 a thread hold the row; NC = 0: a longer row, read twice.
@@ -139,17 +167,24 @@ __global__ void __launch_bounds__(NT) quantize_kernel(int32_t k, const void* __r
   // 0 with eps 0 or leaves fp32
   const bool bad = !(top < INFINITY) || (F == kNorm && !(ss < INFINITY && f < INFINITY));
   const float s = bad ? __uint_as_float(0x7FC00000u) : top / 127.f;
-  const bool none = bad || s == 0.f;
   if (tid == 0) scales[row] = s;
+  // behind the norm y is x * gain: the row's factor goes into the quotient's divisor
+  const float raw = F == kNorm ? __uint_as_float(m) / 127.f : s, r = 1.f / raw;
+  const bool none = bad || raw == 0.f || s == 0.f;
+  const bool near = raw > 1e-30f && raw < 1e30f;
+  auto codes = [&](const float (&v)[8]) {
+    if (none) return u32x2{0, 0};
+    return near ? codes8<F == kRowsBf16 || F == kRowsF32>(v, raw, r) : codes8_far(v, raw);
+  };
   uint8_t* out = q + row * k;
   if constexpr (NC > 0) {
 #pragma unroll
     for (int i = 0; i < NC; ++i)
-      if (tid + i * NT < chunks) *(u32x2*)(out + (tid + i * NT) * 8) = codes8(y[i], f, s, none);
+      if (tid + i * NT < chunks) *(u32x2*)(out + (tid + i * NT) * 8) = codes(y[i]);
   } else {
     for (int c = tid; c < chunks; c += NT) {
       load8<F>(x, gain, row, k, c * 8, y[0], ss);
-      *(u32x2*)(out + c * 8) = codes8(y[0], f, s, none);
+      *(u32x2*)(out + c * 8) = codes(y[0]);
     }
   }
 }

@@ -94,6 +94,9 @@ class OnDevice(torch.Tensor):
     is_cuda = True
     device = torch.device("cuda", 0)
 
+    def get_device(self):
+        return 0
+
 
 def _new(*shape, dtype=torch.int8):
     return torch.zeros(*shape, dtype=dtype).as_subclass(OnDevice)
@@ -136,6 +139,9 @@ def test_the_binding_checks_a_product(change, calls, monkeypatch):
         assert calls[0][1][:3] == (5, 24, 32) and calls[0][1][3:9] == tuple(t.data_ptr() for t in (x, xs, w, ws, r, out))
         with pytest.raises(ValueError):
             int8.gemm_int8_multi(x, xs, [w], [ws, ws], [out], stream=STREAM)
+        calls.clear()
+        int8.gemm_int8_multi(x, xs, [], [], [], stream=STREAM)       # the library refuses the count
+        assert calls[0][1][2] == 0
 
 
 def test_the_binding_checks_rows(calls, monkeypatch):
