@@ -29,6 +29,7 @@
 #include <utility>
 
 #include "elementwise.h"
+#include "gemm_int8.h"
 #include "internal.h"
 
 // The requests write M0 (the LDS address of a global->LDS load) from inline
@@ -60,18 +61,6 @@ template <int N>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
-
-// Up to three products of the same X; their tile columns are numbered through.
-struct Int8Args {
-  int m, k, count;
-  const uint8_t* x;
-  const float* xs;
-  const uint8_t* w[kGemmMulti];
-  const float* ws[kGemmMulti];
-  const uint16_t* r[kGemmMulti];
-  uint16_t* y[kGemmMulti];
-  int n[kGemmMulti];
-};
 
 // ONCE: one tile row, so no other tile reads this W: non-temporal requests.
 template <int BM, int BN, int WGM, int WGN, int KSUB, int NST, int GS, int GM, bool ONCE>
@@ -105,21 +94,8 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) gemm_int8_ring_kernel(Int8A
   const int idx = t - grp * GM * n_tn;
   const int m0 = (first_m + idx % gsize) * BM;
   int tn = idx / gsize;
-  const uint8_t* W = a.w[0];
-  const float* WS = a.ws[0];
-  const uint16_t* R = a.r[0];
-  uint16_t* Y = a.y[0];
-  int N = a.n[0];
-#pragma unroll
-  for (int i = 1; i < kGemmMulti; ++i)
-    if (i < a.count && tn >= (N + BN - 1) / BN) {
-      tn -= (N + BN - 1) / BN;
-      W = a.w[i];
-      WS = a.ws[i];
-      R = a.r[i];
-      Y = a.y[i];
-      N = a.n[i];
-    }
+  const Int8Side p = int8_side<BN>(a, tn);
+  const int N = p.n;
   const int n0 = tn * BN;
 
   const int tid = threadIdx.x;
@@ -130,7 +106,7 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) gemm_int8_ring_kernel(Int8A
   // This lane's requests: run j holds rows 8 (w + NW j) + lane / 8; rows past M or
   // N read row M-1 or N-1 (never stored).  Offsets from the tile's first row.
   const char* const X0 = (const char*)a.x + (int64_t)m0 * K;
-  const char* const W0 = (const char*)W + (int64_t)n0 * K;
+  const char* const W0 = (const char*)p.w + (int64_t)n0 * K;
   uint32_t xrow[XR], wrow[WR];
   int xc[XR], wc[WR];                              // chunk of the image row this lane fetches
 #pragma unroll
@@ -260,26 +236,33 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) gemm_int8_ring_kernel(Int8A
   }
   if (s < nst) stage(s, std::integral_constant<int, 0>{});
 
-  // acc[i][j] lane l, register q: n = wn + 16 i + 4 (l / 16) + q, m = wm + 16 j + l % 16
+  // acc[i][j] lane l, register q: n = wn + 16 i + 4 (l / 16) + q, m = wm + 16 j + l % 16.
+  // Scales, and a row's residuals, are asked for ahead of the stores that could (as far
+  // as the compiler knows) change them.
+  const int nb = n0 + wn + 4 * g4;                 // N is a multiple of 8: whole groups in or out
+  f32x4 wsc[TN];
+#pragma unroll
+  for (int i = 0; i < TN; ++i) wsc[i] = *(const f32x4*)(p.ws + min(nb + 16 * i, N - 4));
+  float xsc[TM];
+#pragma unroll
+  for (int j = 0; j < TM; ++j) xsc[j] = a.xs[min(m0 + wm + 16 * j + r16, M - 1)];
 #pragma unroll
   for (int j = 0; j < TM; ++j) {
     const int m = m0 + wm + 16 * j + r16;
     if (m >= M) continue;
-    const float xsc = a.xs[m];
+    const int64_t row = (int64_t)m * N;
+    u32x2 rb[TN];
+    if (p.r) {
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+        if (nb + 16 * i < N) rb[i] = *(const u32x2*)(p.r + row + nb + 16 * i);
+    }
 #pragma unroll
     for (int i = 0; i < TN; ++i) {
-      const int n = n0 + wn + 16 * i + 4 * g4;
-      if (n >= N) continue;                        // N is a multiple of 8: whole group in or out
-      const int64_t o = (int64_t)m * N + n;
-      f32x4 v = __builtin_convertvector(acc[i][j], f32x4) * (xsc * *(const f32x4*)(WS + n));
-      if (R) {
-        const u32x2 rb = *(const u32x2*)(R + o);
-        v[0] += lo_bf16(rb[0]);
-        v[1] += hi_bf16(rb[0]);
-        v[2] += lo_bf16(rb[1]);
-        v[3] += hi_bf16(rb[1]);
-      }
-      *(bf16x4*)(Y + o) = __builtin_convertvector(v, bf16x4);
+      if (nb + 16 * i >= N) continue;
+      f32x4 v = __builtin_convertvector(acc[i][j], f32x4) * (xsc[j] * wsc[i]);
+      if (p.r) v += f32x4{lo_bf16(rb[i][0]), hi_bf16(rb[i][0]), lo_bf16(rb[i][1]), hi_bf16(rb[i][1])};
+      *(bf16x4*)(p.y + row + nb + 16 * i) = __builtin_convertvector(v, bf16x4);
     }
   }
 }
@@ -297,31 +280,51 @@ void launch_ring(const Int8Args& a, hipStream_t s) {
 }
 
 // Tile choice: the time of a launch is close to
-//   max(1, 0.36 r + 0.64 ceil(r)) * (K / 128) * step,   r = tiles / 256 CUs
-// (a partly filled last round costs most of a whole one).
+//   max(1, 0.36 r + 0.64 ceil(r)) * (K / 128 * step + fix),   r = tiles / 256 CUs
+// (a partly filled last round costs most of a whole one): one 128-k step of one tile
+// per CU, and a tile's prologue and epilogue.  step and fix are the fit to 148 products
+// (M 1 to 4096; N and K of three models' projections and smaller ones, W out of the
+// caches), where the tile it picks is 1.1% slower than the fastest of the nine on
+// average and 13% at most (102 x 4096 x 4096 in 64 x 32 tiles 9.5 us, 32 x 32 8.4).
 struct TileCost {
   int bm, bn;
-  double step_ns;
+  double step_ns, fix_ns;
 };
-constexpr TileCost kTiles[] = {{16, 16, 68},   {32, 16, 112},  {32, 32, 122},   {64, 32, 172},
-                               {64, 64, 277}, {128, 64, 350}, {128, 128, 538}, {256, 128, 885}};
-constexpr int kTileCount = 8;
+constexpr TileCost kTiles[] = {{16, 16, 64, 837},     {32, 16, 87, 1737},    {32, 32, 107, 1129},
+                               {64, 32, 162, 2156},   {64, 64, 229, 2197},   {128, 64, 348, 1912},
+                               {128, 128, 601, 1587}, {256, 128, 963, 1731}, {256, 256, 1504, 674}};
+constexpr int kWide = 8;               // gemm_int8_wide.hip; K a multiple of 128
 
-int pick_tile(int m, int count, const int* n) {
+int pick_tile(int m, int k, int count, const int* n) {
   int best = 0;
   double best_cost = 0;
-  for (int i = 0; i < kTileCount; ++i) {
+  for (int i = 0; i <= (k % 128 == 0 ? kWide : kWide - 1); ++i) {
     const TileCost& t = kTiles[i];
     double cols = 0;
     for (int j = 0; j < count; ++j) cols += ((int64_t)n[j] + t.bn - 1) / t.bn;
     const double r = (double)(((int64_t)m + t.bm - 1) / t.bm) * cols / kCus;
-    const double cost = t.step_ns * (r <= 1.0 ? 1.0 : 0.36 * r + 0.64 * ceil(r));
+    const double cost = (r <= 1.0 ? 1.0 : 0.36 * r + 0.64 * ceil(r)) * ((k + 127) / 128 * t.step_ns + t.fix_ns);
     if (i == 0 || cost < best_cost) {
       best = i;
       best_cost = cost;
     }
   }
   return best;
+}
+
+hipError_t run_tile(int tile, const Int8Args& a, hipStream_t s) {
+  switch (tile) {
+    case 0: launch_ring<16, 16, 1, 1, 2, 8, 4, 8>(a, s); break;
+    case 1: launch_ring<32, 16, 2, 1, 2, 8, 4, 8>(a, s); break;
+    case 2: launch_ring<32, 32, 2, 2, 2, 4, 4, 8>(a, s); break;
+    case 3: launch_ring<64, 32, 2, 2, 2, 6, 2, 8>(a, s); break;
+    case 4: launch_ring<64, 64, 2, 2, 2, 4, 2, 8>(a, s); break;
+    case 5: launch_ring<128, 64, 4, 2, 2, 3, 2, 8>(a, s); break;
+    case 6: launch_ring<128, 128, 4, 2, 1, 4, 1, 8>(a, s); break;
+    case 7: launch_ring<256, 128, 4, 2, 1, 3, 1, 4>(a, s); break;
+    default: return launch_gemm_int8_wide(a, s);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -351,17 +354,7 @@ hipError_t launch_gemm_int8(int m, int k, int count, const int* n, const void* x
   }
   if (m <= 0 || a.count == 0) return hipSuccess;
   a.r[0] = (const uint16_t*)r;
-  switch (pick_tile(m, a.count, a.n)) {
-    case 0: launch_ring<16, 16, 1, 1, 2, 8, 4, 8>(a, s); break;
-    case 1: launch_ring<32, 16, 2, 1, 2, 8, 4, 8>(a, s); break;
-    case 2: launch_ring<32, 32, 2, 2, 2, 4, 4, 8>(a, s); break;
-    case 3: launch_ring<64, 32, 2, 2, 2, 6, 2, 8>(a, s); break;
-    case 4: launch_ring<64, 64, 2, 2, 2, 4, 2, 8>(a, s); break;
-    case 5: launch_ring<128, 64, 4, 2, 2, 3, 2, 8>(a, s); break;
-    case 6: launch_ring<128, 128, 4, 2, 1, 4, 1, 8>(a, s); break;
-    default: launch_ring<256, 128, 4, 2, 1, 3, 1, 4>(a, s); break;
-  }
-  return hipGetLastError();
+  return run_tile(pick_tile(m, k, a.count, a.n), a, s);
 }
 
 }  // namespace pgsr
