@@ -161,6 +161,19 @@ attn_bf16_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t*
     if constexpr (kBlkConst) return tid + (i % (CHB / NT)) * NT;
     else return tid % CHB;
   };
+  // V of an int8 cache: a thread's chunks hold the same eight keys, so that their
+  // exponents are read and taken apart once.
+  constexpr bool kVShare = CK == kCacheInt8;
+  constexpr int VT = CHB / CPT;            // threads to a block-head
+  static_assert(!kVShare || (VT % 64 == 0 && VT % (B / 8) == 0), "a block for each wave, a key group for each thread");
+  auto vchunk_blk = [&](int i) {
+    if constexpr (kVShare) return __builtin_amdgcn_readfirstlane(tid / VT);
+    else return chunk_blk(i);
+  };
+  auto vchunk_in = [&](int i) {
+    if constexpr (kVShare) return tid % VT + i * VT;
+    else return chunk_in(i);
+  };
 
   // Block ids of a key tile, clamped in range.  They are fetched as a
   // per-lane vector load (lane bi holds block bi's id) one tile before use,
@@ -180,19 +193,20 @@ attn_bf16_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t*
   };
 
   Raw kreg[CPT], vreg[CPT];
-  uint32_t kexp[CK == kCacheInt8 ? CPT : 1];       // int8: a K chunk's exponent, a V chunk's eight
-  u32x2 vexp[CK == kCacheInt8 ? CPT : 1];
+  uint32_t kexp[CK == kCacheInt8 ? CPT : 1];       // int8: each K chunk's exponent, the V chunks' eight
+  u32x2 vexp;
   auto load_tile = [&](const Ids& ids) {
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
       const int in = chunk_in(i);
-      const int64_t base = (head_base + (int64_t)ids.get(chunk_blk(i)) * hkv) * (B * D);
-      kreg[i] = *(const Raw*)(kc + base + (in / (D / 8)) * D + (in % (D / 8)) * 8);
-      vreg[i] = *(const Raw*)(vc + base + (in / (B / 8)) * B + (in % (B / 8)) * 8);
+      const int64_t head = head_base + (int64_t)ids.get(chunk_blk(i)) * hkv;
+      const int64_t vhead = kVShare ? head_base + (int64_t)ids.get(vchunk_blk(i)) * hkv : head;
+      const int vin = vchunk_in(i);
+      kreg[i] = *(const Raw*)(kc + head * (B * D) + (in / (D / 8)) * D + (in % (D / 8)) * 8);
+      vreg[i] = *(const Raw*)(vc + vhead * (B * D) + (vin / (B / 8)) * B + (vin % (B / 8)) * 8);
       if constexpr (CK == kCacheInt8) {
-        const uint8_t* xp = a.kv_exps + (head_base + (int64_t)ids.get(chunk_blk(i)) * hkv) * (2 * B);
-        kexp[i] = xp[in / (D / 8)];
-        vexp[i] = *(const u32x2*)(xp + B + (in % (B / 8)) * 8);
+        kexp[i] = a.kv_exps[head * (2 * B) + in / (D / 8)];
+        if (i == 0) vexp = *(const u32x2*)(a.kv_exps + vhead * (2 * B) + B + (vin % (B / 8)) * 8);
       }
     }
   };
@@ -203,7 +217,7 @@ attn_bf16_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t*
   };
   auto v_bf16 = [&](int i) {
     if constexpr (CK == kCacheFp8) return widen_fp8(vreg[i]);
-    else if constexpr (CK == kCacheInt8) return widen_int8(vreg[i], vexp[i]);
+    else if constexpr (CK == kCacheInt8) return widen_int8(vreg[i], vexp);
     else return vreg[i];
   };
   auto store_tile = [&](int buf, int kb) {
@@ -212,7 +226,8 @@ attn_bf16_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t*
     for (int i = 0; i < CPT; ++i) {
       const int blk = chunk_blk(i), in = chunk_in(i);
       *(u32x4*)&k_lds[buf][(blk * B + in / (D / 8)) * KLD + (in % (D / 8)) * 8] = k_bf16(i);
-      const int dd = in / (B / 8), key0 = blk * B + (in % (B / 8)) * 8;
+      const int vin = vchunk_in(i);
+      const int dd = vin / (B / 8), key0 = vchunk_blk(i) * B + (vin % (B / 8)) * 8;
       u32x4 val = v_bf16(i);
       if (tail) {
         const int pos0 = kb + key0;

@@ -167,6 +167,20 @@ attn_bf16_pipe_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint
     if constexpr (kBlkConst) return tid + (i % (CHB / NT)) * NT;
     else return tid % CHB;
   };
+  // V of an int8 cache: a thread's chunks hold the same eight keys, so that their
+  // exponents are read and taken apart once.
+  constexpr bool kVShare = CK == kCacheInt8;
+  constexpr int VT = CHB / CPT;            // threads to a block-head
+  static_assert(!kVShare || (VT % 64 == 0 && VT % (B / 8) == 0), "a block for each wave, a key group for each thread");
+  const int wave_vblk = __builtin_amdgcn_readfirstlane(tid / VT);
+  auto vchunk_blk = [&](int i) {
+    if constexpr (kVShare) return wave_vblk;
+    else return chunk_blk(i);
+  };
+  auto vchunk_in = [&](int i) {
+    if constexpr (kVShare) return tid % VT + i * VT;
+    else return chunk_in(i);
+  };
   // Block ids of a tile: a per-lane load (lane bi holds block bi's id) one
   // step ahead; each chunk reads its block's id with readlane at a scalar
   // lane index.
@@ -182,11 +196,12 @@ attn_bf16_pipe_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint
   for (int i = 0; i < CPT; ++i) {
     const int in = chunk_in(i);
     koff[i] = (in / (D / 8)) * D + (in % (D / 8)) * 8;
-    voff[i] = (in / (B / 8)) * B + (in % (B / 8)) * 8;
+    const int vin = vchunk_in(i);
+    voff[i] = (vin / (B / 8)) * B + (vin % (B / 8)) * 8;
   }
   Raw kreg[CPT], vreg[CPT];
-  uint32_t kexp[CK == kCacheInt8 ? CPT : 1];       // int8: a K chunk's exponent, a V chunk's eight
-  u32x2 vexp[CK == kCacheInt8 ? CPT : 1];
+  uint32_t kexp[CK == kCacheInt8 ? CPT : 1];       // int8: each K chunk's exponent, the V chunks' eight
+  u32x2 vexp;
   auto k_bf16 = [&](int i) {
     if constexpr (CK == kCacheFp8) return widen_fp8(kreg[i]);
     else if constexpr (CK == kCacheInt8) return widen_int8(kreg[i], __uint_as_float(kexp[i] << 23));
@@ -194,7 +209,7 @@ attn_bf16_pipe_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint
   };
   auto v_bf16 = [&](int i) {
     if constexpr (CK == kCacheFp8) return widen_fp8(vreg[i]);
-    else if constexpr (CK == kCacheInt8) return widen_int8(vreg[i], vexp[i]);
+    else if constexpr (CK == kCacheInt8) return widen_int8(vreg[i], vexp);
     else return vreg[i];
   };
   auto load_tile = [&](int ids) {
@@ -203,11 +218,14 @@ attn_bf16_pipe_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint
       const int id = __builtin_amdgcn_readlane(ids, chunk_blk(i));
       const int64_t base = (head_base + (int64_t)id * hkv) * (B * D);
       kreg[i] = *(const Raw*)((kc + base) + koff[i]);
-      vreg[i] = *(const Raw*)((vc + base) + voff[i]);
       if constexpr (CK == kCacheInt8) {
-        const uint8_t* xp = a.kv_exps + (head_base + (int64_t)id * hkv) * (2 * B);
-        kexp[i] = xp[chunk_in(i) / (D / 8)];
-        vexp[i] = *(const u32x2*)(xp + B + (chunk_in(i) % (B / 8)) * 8);
+        kexp[i] = a.kv_exps[(head_base + (int64_t)id * hkv) * (2 * B) + chunk_in(i) / (D / 8)];
+        const int vid = __builtin_amdgcn_readlane(ids, vchunk_blk(i));
+        const int64_t vhead = head_base + (int64_t)vid * hkv;
+        vreg[i] = *(const Raw*)((vc + vhead * (B * D)) + voff[i]);
+        if (i == 0) vexp = *(const u32x2*)(a.kv_exps + vhead * (2 * B) + B + (vchunk_in(0) % (B / 8)) * 8);
+      } else {
+        vreg[i] = *(const Raw*)((vc + base) + voff[i]);
       }
     }
   };
@@ -217,7 +235,8 @@ attn_bf16_pipe_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint
     for (int i = 0; i < CPT; ++i) {
       const int blk = chunk_blk(i), in = chunk_in(i);
       *(u32x4*)&k_lds[buf][(blk * B + in / (D / 8)) * KLD + (in % (D / 8)) * 8] = k_bf16(i);
-      const int dd = in / (B / 8), key0 = blk * B + (in % (B / 8)) * 8;
+      const int vin = vchunk_in(i);
+      const int dd = vin / (B / 8), key0 = vchunk_blk(i) * B + (vin % (B / 8)) * 8;
       u32x4 val = v_bf16(i);
       if (tail) val = zero_tail(val, kb + key0, kv_len);   // selects only: no per-lane branch
       *(u32x4*)&v_lds[buf][dd * VLD + key0] = val;
