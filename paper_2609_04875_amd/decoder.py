@@ -7,15 +7,30 @@ rotates exactly as the full run); attention through the paged pool (one pool
 layer per model layer); x <- x + O Wo; h2 = RMSNorm(x) g_mlp;
 x <- x + (SiLU(h2 Wg) * (h2 Wu)) Wd.  Every step is a library call; this
 module only sequences them and owns scratch tensors.
+
+Weights may be int8 codes with a scale for each output channel
+(``quantize_weights``): the projections then run on 8-bit integers, their left
+operands quantised a token at a time behind the norms, the attention and the
+gate.  The cache may be int8 or FP8 whatever the weights are.
 """
 from __future__ import annotations
 
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
 
 from . import _native as N
+from .int8 import gemm_int8, gemm_int8_multi, quantize_rows, rmsnorm_int8, silu_mul_int8
 from .pool import KVPool, _dev_ptr, gemm_bf16, gemm_bf16_multi, gemm_silu_bf16
+
+PROJECTIONS = ("wq", "wk", "wv", "wo", "w_gate_up", "w_down")
+Weight = Union[torch.Tensor, Tuple[torch.Tensor, torch.Tensor]]
+
+
+def quantize_weights(weights: Sequence[Dict[str, torch.Tensor]]) -> List[Dict[str, Weight]]:
+    """The weights of ``DecoderReplay`` with every projection as int8 codes and a
+    fp32 scale for each output channel; the gains stay bf16."""
+    return [{name: quantize_rows(w) if name in PROJECTIONS else w for name, w in layer.items()} for layer in weights]
 
 
 def _stream(stream):
@@ -56,54 +71,79 @@ def silu_mul(gate_up: torch.Tensor, out: Optional[torch.Tensor] = None, stream=N
 
 
 class DecoderReplay:
-    def __init__(self, weights: Sequence[Dict[str, torch.Tensor]], n_q_heads: int, n_kv_heads: int,
+    def __init__(self, weights: Sequence[Dict[str, Weight]], n_q_heads: int, n_kv_heads: int,
                  head_dim: int, eps: float, theta: float, n_blocks: int, max_seqs: int,
-                 max_blocks_per_seq: int, block_size: int = 16, workspace_bytes: int = 0):
+                 max_blocks_per_seq: int, block_size: int = 16, workspace_bytes: int = 0,
+                 kv_dtype: int = N.BF16):
         """``weights``: per layer a dict of bf16 CUDA tensors in the linear-layer
         [out][in] layout: wq [Hq*d, dm], wk, wv [Hkv*d, dm], wo [dm, Hq*d],
         w_gate_up [2*d_ff, dm] (gate rows then up rows), w_down [dm, d_ff],
-        and the gains g_attn, g_mlp [dm]."""
+        and the gains g_attn, g_mlp [dm]; or the same through
+        ``quantize_weights``.  ``kv_dtype``: the cache's, BF16, FP8_E4M3 or INT8."""
         self.w = list(weights)
+        kinds = {isinstance(layer[name], tuple) for layer in self.w for name in PROJECTIONS}
+        if len(kinds) != 1:
+            raise ValueError("projections must all be bf16 tensors or all int8 codes with scales")
+        if kv_dtype not in (N.BF16, N.FP8_E4M3, N.INT8):
+            raise ValueError(f"kv_dtype {kv_dtype}: the layers' states are bf16")
+        self.int8 = kinds.pop()
         self.hq, self.hkv, self.d, self.eps, self.theta = n_q_heads, n_kv_heads, head_dim, eps, theta
-        self.d_model = self.w[0]["wq"].shape[1]
-        self.d_ff = self.w[0]["w_down"].shape[1]
+        wq, w_down = (w[0] if self.int8 else w for w in (self.w[0]["wq"], self.w[0]["w_down"]))
+        self.d_model, self.d_ff = wq.shape[1], w_down.shape[1]
         self.pool = KVPool(len(self.w), n_q_heads, n_kv_heads, head_dim, n_blocks, max_seqs,
-                           max_blocks_per_seq, N.BF16, block_size, workspace_bytes=workspace_bytes)
+                           max_blocks_per_seq, kv_dtype, block_size, workspace_bytes=workspace_bytes)
         self._buf: Dict[str, torch.Tensor] = {}
 
-    def _scratch(self, name: str, *shape) -> torch.Tensor:
-        n = 1
-        for s in shape:
-            n *= s
-        t = self._buf.get(name)
-        if t is None or t.numel() < n:
-            t = self._buf[name] = torch.empty(n, dtype=torch.bfloat16, device="cuda")
-        return t[:n].view(*shape)
+    def _scratch_of(self, n: int) -> Dict[str, torch.Tensor]:
+        """Scratch tensors of ``n`` tokens, by name."""
+        bf, i8, f32 = torch.bfloat16, torch.int8, torch.float32
+        want = {"q": (bf, n, self.hq, self.d), "k": (bf, n, self.hkv, self.d), "v": (bf, n, self.hkv, self.d),
+                "o": (bf, n, self.hq * self.d), "gu": (bf, n, 2 * self.d_ff)}
+        if self.int8:      # codes and scales of the left operands
+            want.update(hq=(i8, n, self.d_model), oq=(i8, n, self.hq * self.d), aq=(i8, n, self.d_ff), s=(f32, n))
+        else:
+            want.update(h=(bf, n, self.d_model), a=(bf, n, self.d_ff))
+        out = {}
+        for name, (dtype, *shape) in want.items():
+            size = 1
+            for x in shape:
+                size *= x
+            t = self._buf.get(name)
+            if t is None or t.numel() < size:
+                t = self._buf[name] = torch.empty(size, dtype=dtype, device="cuda")
+            out[name] = t[:size].view(*shape)
+        return out
 
     def _run(self, fn, seq: int, x: torch.Tensor, pos0: int) -> torch.Tensor:
         n = x.shape[0]
         pos = torch.arange(pos0, pos0 + n, dtype=torch.int32, device="cuda")
-        h = self._scratch("h", n, self.d_model)
-        q = self._scratch("q", n, self.hq, self.d)
-        k = self._scratch("k", n, self.hkv, self.d)
-        v = self._scratch("v", n, self.hkv, self.d)
-        o = self._scratch("o", n, self.hq * self.d)
-        gu = self._scratch("gu", n, 2 * self.d_ff)
-        a = self._scratch("a", n, self.d_ff)
+        b = self._scratch_of(n)
+        q, k, v, o, gu = (b[name] for name in ("q", "k", "v", "o", "gu"))
         x = x.clone()
         scale = self.d ** -0.5
         last = len(self.w) - 1
         for li, w in enumerate(self.w):
-            rmsnorm(x, w["g_attn"], self.eps, out=h)
-            gemm_bf16_multi(h, (w["wq"], w["wk"], w["wv"]), (q, k, v))
+            qkv = (w["wq"], w["wk"], w["wv"])
+            if self.int8:
+                rows = rmsnorm_int8(x, w["g_attn"], self.eps, out=b["hq"], scales=b["s"])
+                gemm_int8_multi(*rows, [c for c, _ in qkv], [s for _, s in qkv], (q, k, v))
+            else:
+                rmsnorm(x, w["g_attn"], self.eps, out=b["h"])
+                gemm_bf16_multi(b["h"], qkv, (q, k, v))
             rope_qk_(q, k, pos, self.theta)
             rc = fn(li, [seq], [n], q, k, v, o, scale, commit=(li == last))
             if rc:
                 raise N.PgsrError(rc, N.lib.pgsr_last_error().decode())
-            gemm_bf16(o, w["wo"], r=x, out=x)                 # x <- x + O Wo
-            rmsnorm(x, w["g_mlp"], self.eps, out=h)
-            gemm_silu_bf16(h, w["w_gate_up"], gu, a)
-            gemm_bf16(a, w["w_down"], r=x, out=x)             # x <- x + MLP(x)
+            if self.int8:
+                gemm_int8(*quantize_rows(o, out=b["oq"], scales=b["s"]), *w["wo"], r=x, out=x)
+                rows = rmsnorm_int8(x, w["g_mlp"], self.eps, out=b["hq"], scales=b["s"])
+                gemm_int8(*rows, *w["w_gate_up"], out=gu)
+                gemm_int8(*silu_mul_int8(gu, out=b["aq"], scales=b["s"]), *w["w_down"], r=x, out=x)
+            else:
+                gemm_bf16(o, w["wo"], r=x, out=x)                 # x <- x + O Wo
+                rmsnorm(x, w["g_mlp"], self.eps, out=b["h"])
+                gemm_silu_bf16(b["h"], w["w_gate_up"], gu, b["a"])
+                gemm_bf16(b["a"], w["w_down"], r=x, out=x)        # x <- x + MLP(x)
         return x
 
     def replay(self, seq: int, x: torch.Tensor) -> torch.Tensor:
@@ -133,10 +173,7 @@ class DecoderReplay:
         # grow the shared scratch must not free them
         shared, self._buf = self._buf, {}
         try:
-            for name, shape in (("h", (n, self.d_model)), ("q", (n, self.hq, self.d)),
-                                ("k", (n, self.hkv, self.d)), ("v", (n, self.hkv, self.d)),
-                                ("o", (n, self.hq * self.d)), ("gu", (n, 2 * self.d_ff)), ("a", (n, self.d_ff))):
-                self._scratch(name, *shape)
+            self._scratch_of(n)
             xin = x.clone()
             stream = torch.cuda.Stream()
             stream.wait_stream(torch.cuda.current_stream())
