@@ -323,20 +323,24 @@ int pgsr_pool_last_clock(pgsr_pool *pool, void *stream, double *ghz, int64_t *cy
  *    of the call past 130816 keys (prefix + suffix): the wide kernel (one wave per
  *    SIMD, 64 query rows per wave, global->LDS tile loads) or, for calls that
  *    leave CUs idle, the narrow one (32 query rows per wave);
- *  - other bf16 pools and FP8 pools: the software-pipelined kernel (32 query rows
- *    per wave, two waves per SIMD) or, for calls that leave CUs idle, with one
- *    wave per SIMD (FP8) or the four-wave kernel (bf16);
+ *  - other bf16 pools, FP8 and int8 pools: the software-pipelined kernel (32 query
+ *    rows per wave, two waves per SIMD) or, for calls that leave CUs idle, with one
+ *    wave per SIMD (FP8, int8) or the four-wave kernel (bf16);
+ *  - int8 pools, calls that fill the chip and read every key in five tiles or more,
+ *    with a workspace of 512 bytes per KV head and token and a table (4 bytes per 16
+ *    tokens of the longest sequence, for each sequence): the wide kernel on a bf16
+ *    copy of the call's keys and values that the workspace takes;
  *  - the four-wave kernel for batches whose sequences fill the larger tiles badly
- *    (FP8, and groups G = n_q_heads / n_kv_heads that do not divide 32), for
- *    calls with split keys of such groups in bf16, and for those of FP8 pools whose
- *    larger tiles do not all have a CU.
+ *    (FP8, int8 and groups G = n_q_heads / n_kv_heads that do not divide 32), for
+ *    calls with split keys of such groups in bf16, and for those of FP8 and int8
+ *    pools whose larger tiles do not all have a CU.
  * PGSR_PREFILL_PIPELINED runs the pipelined kernel with two waves per SIMD, but for
  * bf16 calls with split keys of a group that does not divide 32, which stay with
  * the four-wave kernel.  PGSR_PREFILL_FOUR_WAVE runs the four-wave kernel.
  *
  * All kernels give identical bits for every query row of calls that are not split
  * (no workspace, or enough workgroups without).  Splits round: their number is the
- * same under every choice for FP8 pools and for groups that do not divide 32, and
+ * same under every choice for FP8 and int8 pools and for groups that do not divide 32, and
  * under AUTO and PIPELINED for the others, where FOUR_WAVE cuts for its own tiles.
  * Host only, no device work; EINVAL for another value.
  */

@@ -241,6 +241,28 @@ hipError_t launch_append(const AppendArgs& a, int elem_bytes, hipStream_t s);
 // and the append of an int8 pool, which quantises a row of each token and KV head.
 hipError_t launch_cow(const AppendArgs& a, int elem_bytes, hipStream_t s);
 hipError_t launch_append_int8(const AppendArgs& a, hipStream_t s);
+// An int8 cache's keys and values of some sequences as a bf16 cache of 16-token
+// blocks (head_dim 128), block ids counting up from 0: k [block][KV head][16][128],
+// v [block][KV head][128][16], out_tables [n][out_bps] (row i: entry i).
+struct ExpandEntry {
+  int32_t seq, kv_len;
+  int32_t blk_start;      // prefix sum of 16-token blocks
+};
+struct ExpandArgs {
+  const void* k_cache;
+  const void* v_cache;
+  const uint8_t* kv_exps;
+  const int32_t* tables;
+  int32_t* chk;
+  int32_t max_bps, n_blocks, n_kv_heads, block_size, layer;
+  uint16_t* k_out;
+  uint16_t* v_out;
+  int32_t* out_tables;
+  int32_t out_bps, out_blocks;
+  int32_t n;
+  ExpandEntry e[kMaxSeqsPerLaunch];
+};
+hipError_t launch_expand_int8(const ExpandArgs& a, hipStream_t s);
 // False when the fused launch does not cover this geometry (the caller then
 // launches crop and append separately).
 bool fused_append_supported(int block_size, int head_dim);

@@ -26,14 +26,12 @@
 // long suffix.
 #include <hip/hip_runtime.h>
 
+#include "attn_common.h"
 #include "internal.h"
 
 namespace pgsr {
 
 namespace {
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
 constexpr int kExpLo = -100, kExpHi = 100;
@@ -179,7 +177,39 @@ void launch_b(const AppendArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL((append_int8_kernel<B, 64>), grid, dim3(kThreads), 0, s, a);
 }
 
+// Codes times their powers of two, exact in bf16: a workgroup takes one 16-token block
+// of one KV head, eight values a thread of K and of V.  Bound by HBM: 2 bytes read and
+// 4 written a value pair (10237 tokens x 8 heads 63 MB, 15 us).
+__global__ void __launch_bounds__(kThreads) expand_int8_kernel(ExpandArgs a) {
+  constexpr int D = 128;
+  const int blk = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  static_assert(kMaxSeqsPerLaunch <= 64, "one entry per lane");
+  const int ei = __popcll(__ballot(lane < a.n && a.e[min(lane, a.n - 1)].blk_start <= blk)) - 1;
+  const ExpandEntry e = a.e[ei];
+  const int lb = blk - e.blk_start, B = a.block_size, slot0 = lb * 16 % B;
+  const int32_t id = blk_id(a.tables[(int64_t)e.seq * a.max_bps + lb * 16 / B], a.n_blocks, a.chk);
+  if (h == 0 && tid == 0) a.out_tables[(int64_t)ei * a.out_bps + lb] = blk;
+  const int64_t head = ((int64_t)a.layer * a.n_blocks + id) * a.n_kv_heads + h;
+  const int64_t out = ((int64_t)blk * a.n_kv_heads + h) * 16 * D;
+  const uint8_t *kc = (const uint8_t*)a.k_cache + head * B * D, *vc = (const uint8_t*)a.v_cache + head * D * B;
+  const uint8_t* ex = a.kv_exps + head * 2 * B + slot0;
+  const int t = tid / 16, c = tid % 16 * 8;        // K: slot, column
+  const int d = tid / 2, half = tid % 2 * 8;       // V: row, slots
+  const u32x2 kw = *(const u32x2*)(kc + (slot0 + t) * D + c);
+  const u32x2 vw = *(const u32x2*)(vc + d * B + slot0 + half);
+  const uint32_t ke = ex[t];
+  const u32x2 ve = *(const u32x2*)(ex + B + half);
+  *(u32x4*)(a.k_out + out + t * D + c) = widen_int8(kw, __uint_as_float(ke << 23));
+  *(u32x4*)(a.v_out + out + d * 16 + half) = widen_int8(vw, ve);
+}
+
 }  // namespace
+
+hipError_t launch_expand_int8(const ExpandArgs& a, hipStream_t s) {
+  if (a.n <= 0 || a.out_blocks <= 0) return hipSuccess;
+  hipLaunchKernelGGL(expand_int8_kernel, dim3(a.out_blocks, a.n_kv_heads), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
 
 hipError_t launch_append_int8(const AppendArgs& a, hipStream_t s) {
   if (a.n <= 0 || a.n_items <= 0) return hipSuccess;

@@ -369,6 +369,41 @@ struct FoldedCrop {
   CropEntry e[kMaxFusedSeqs];
 };
 
+// Lays a bf16 copy of the entries' keys and values (16-token blocks) into the
+// workspace: false where it has no room or the wide kernel does not take it.
+bool plan_expand(const pgsr_pool* p, const AttnArgs& a, void* ws, size_t ws_bytes, ExpandArgs& x) {
+  int64_t blocks = 0, bps = 0, max_kv = 0;
+  for (int32_t i = 0; i < a.n; ++i) {
+    const int64_t kv = (int64_t)a.e[i].prefix + a.e[i].q_len, b = cdiv(kv, 16);
+    x.e[i] = {a.e[i].seq, (int32_t)kv, (int32_t)blocks};
+    blocks += b;
+    bps = std::max(bps, b);
+    max_kv = std::max(max_kv, kv);
+    if (blocks > INT32_MAX) return false;
+  }
+  if (!attn_bf16_wide_eligible(p->d, p->hq / p->hkv, 16, blocks, p->hkv, max_kv)) return false;
+  const size_t cache = (size_t)blocks * p->hkv * 16 * p->d * sizeof(uint16_t);
+  const size_t pad = (256 - (uintptr_t)ws % 256) % 256;
+  if (pad + 2 * cache + (size_t)a.n * bps * sizeof(int32_t) > ws_bytes) return false;
+  x.k_cache = a.k_cache;
+  x.v_cache = a.v_cache;
+  x.kv_exps = a.kv_exps;
+  x.tables = a.tables;
+  x.chk = a.chk;
+  x.max_bps = a.max_bps;
+  x.n_blocks = a.n_blocks;
+  x.n_kv_heads = a.n_kv_heads;
+  x.block_size = a.block_size;
+  x.layer = a.layer;
+  x.k_out = (uint16_t*)((char*)ws + pad);
+  x.v_out = (uint16_t*)((char*)x.k_out + cache);
+  x.out_tables = (int32_t*)((char*)x.v_out + cache);
+  x.out_bps = (int32_t)bps;
+  x.out_blocks = (int32_t)blocks;
+  x.n = a.n;
+  return true;
+}
+
 int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
               const int32_t* q_lens, const void* q, const void* k, const void* v, void* o,
               float scale, unsigned flags, int64_t* recomputed, void* ws, size_t ws_bytes,
@@ -621,7 +656,12 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
       int32_t max_key = 0;
       for (int32_t i = 0; i < cnt; ++i) max_key = std::max(max_key, chunk[i].prefix + chunk[i].q_len);
       const int64_t per_split = (int64_t)a.n_rows * ((int64_t)p->d + 2) * (int64_t)sizeof(float);
-      int64_t ns = std::min<int64_t>(kMaxSplits, (target + wgs - 1) / wgs);
+      // Int8 calls of head_dim 128 run the pipelined kernel, whose splits of more than
+      // one workgroup to a CU wait for a second round: rounded down (32 / 8 heads on
+      // 8000 tokens, rounded up and down: 700 tokens 221, 157 us; 1200 333, 220; 100
+      // 42.2, 42.0; head_dim 64, two workgroups to a CU: 49.1, 51.5 and 43.1, 40.8).
+      const bool down = cache == kCacheInt8 && p->d == 128;
+      int64_t ns = std::min<int64_t>(kMaxSplits, (target + (down ? 0 : wgs - 1)) / wgs);
       ns = std::min<int64_t>(ns, (int64_t)(ws_bytes / std::max<int64_t>(per_split, 1)));
       if (ns > 1) {
         const int32_t len = cdiv(cdiv(max_key, ns), kSplitAlign) * kSplitAlign;
@@ -670,7 +710,38 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
     // FP8 calls whose larger tiles all have a CU (450 tokens: 51, pipelined 44).
     int narrow = 0, pipe = 0;       // waves per workgroup of the kernel taken
     bool wide = false;
-    if (p->dtype == PGSR_F32) {
+    // Int8 calls that fill the chip: their keys and values as bf16 in the workspace, if
+    // it has the room, and the wide kernel on those, with the same bits, where each key
+    // is read by five tiles or more: the pipelined kernel converts it in every one (us a
+    // call, 32 / 8 heads, pipelined and through the copy: 2048 tokens on 8189 338, 276;
+    // 2048 on none 86, 72; 64 / 8 heads, 8 x 200 on 3000, seven tiles 219, 195; 8 x 256
+    // on 4000, four 162, 164; 60 x 64 on 3000, one 250, 432).
+    ExpandArgs x{};
+    auto reused = [&] {
+      const int tokens = attn_bf16_pipe_tile_tokens(group, 8);
+      double steps = 0, keys = 0;
+      for (int32_t i = 0; i < cnt; ++i) {
+        const double t = cdiv(chunk[i].q_len, tokens);
+        steps += t * (chunk[i].prefix + 0.5 * chunk[i].q_len);
+        keys += chunk[i].prefix + chunk[i].q_len;
+      }
+      return steps >= 5 * keys;
+    };
+    if (cache == kCacheInt8 && p->prefill_kind == PGSR_PREFILL_AUTO && a.n_splits == 1 && ws_bytes > 0 &&
+        !fits(attn_bf16_narrow_tile_tokens(group, 4)) && reused() && eight_pays(5, 0.75))
+      wide = plan_expand(p, a, ws, ws_bytes, x);
+    if (wide) {
+      hipError_t err = launch_expand_int8(x, st);
+      if (err != hipSuccess) return hip_fail(err, "expand launch");
+      a.k_cache = x.k_out;
+      a.v_cache = x.v_out;
+      a.tables = x.out_tables;
+      a.max_bps = x.out_bps;
+      a.n_blocks = x.out_blocks;
+      a.block_size = 16;
+      a.layer = 0;
+      for (int32_t i = 0; i < cnt; ++i) a.e[i].seq = i;
+    } else if (p->dtype == PGSR_F32) {
       set_tiles(attn_f32_tile_tokens(p->d, group));
     } else if (wide_ok && (split_as_wide || a.n_splits == 1)) {
       narrow = fits(attn_bf16_narrow_tile_tokens(group, 2))   ? 2

@@ -436,3 +436,48 @@ def test_refusals_change_nothing():
     N.lib.pgsr_pool_destroy(h)
     with pytest.raises(ValueError):
         pool.replay(0, [0], [5], *(y.to(torch.int8) for y in x), o, 0.1)
+
+
+# calls that fill the chip without splits and read each key in five tiles or more:
+# geometry, block size, prefixes, suffixes
+EXPAND = [
+    (W.AttnGeometry(32, 8, 128), 16, (1001,), (2100,)),
+    (W.AttnGeometry(32, 8, 128), 64, (277, 100, 640, 315), (1900, 1700, 513, 300)),
+    (W.AttnGeometry(28, 4, 128), 32, (250, 31, 16), (1400, 900, 1500)),
+    (W.AttnGeometry(8, 1, 128), 16, tuple(range(503, 635, 2)), (416,) * 66),
+]
+
+
+@pytest.mark.parametrize("case", range(len(EXPAND)))
+def test_prefill_through_a_bf16_copy_has_the_same_bits(case):
+    """A workspace with the room for the copy, one a byte short of it and none: the
+    copy is made exactly where it fits, and the bits never differ."""
+    geom, B, P, S = EXPAND[case]
+    log(f"int8 prefill through a copy, case {case}")
+    C, d = [p + 40 for p in P], geom.head_dim
+    nb = sum(_blocks(max(c, p + s), B) + 1 for p, s, c in zip(P, S, C))
+    bps = max(_blocks(max(c, p + s), B) for p, s, c in zip(P, S, C)) + 1
+    data, _ = _episodes(np.random.default_rng(70 + case), geom, P, S, C, False)
+    # what the last launch's entries need (64 at most): two caches of 16-token blocks and a table
+    last = [(p + s) for p, s in zip(P, S)][len(P) - (len(P) - 1) % 64 - 1:]
+    need = lambda kv: (2 * 2 * 16 * d * geom.n_kv_heads * sum(_blocks(x) for x in kv)  # noqa: E731
+                       + 4 * len(kv) * max(_blocks(x) for x in kv))
+    first = [(p + s) for p, s in zip(P, S)][:64]
+    from paper_2609_04875_amd import INT8, KVPool
+    outs, used = [], []
+    for ws in (0, need(first) - 1, need(first)):
+        pool = KVPool(1, geom.n_q_heads, geom.n_kv_heads, d, nb, len(P), bps, INT8, B, workspace_bytes=ws)
+        q, k, v, cq, ck, cv = data
+        seqs = list(range(len(P)))
+        assert pool.replay(0, seqs, C, cq, ck, cv, torch.empty_like(cq), 0.09) == 0
+        assert pool.crop(seqs, P, poison=True) == 0
+        if ws:
+            pool.workspace.fill_(0xA5)
+        o = torch.full_like(q, float("nan"))
+        assert pool.replay(0, seqs, S, q, k, v, o, 0.09) == 0
+        torch.cuda.synchronize()
+        outs.append(o)
+        used.append(bool(ws) and bool((pool.workspace[:4096] != 0xA5).any()))
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    assert torch.isfinite(outs[0]).all()
+    assert used[2] and (len(P) > 64 or not used[1])
