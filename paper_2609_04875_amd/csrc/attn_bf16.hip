@@ -422,14 +422,17 @@ __global__ void __launch_bounds__(256) split_combine_kernel(AttnArgs a, TO* __re
   // asks all of them (walking them costs a round through memory each: 32 sequences 8.2
   // us a launch).
   const int lane = threadIdx.x & 63;
-  const AttnEntry mine = a.e[min(lane, a.n - 1)];
-  int qpos = -1;
+  const AttnEntry one = a.e[0];                    // with the first arguments: one entry needs no search
+  int qpos = tok >= one.q_off && tok < one.q_off + one.q_len ? one.prefix + tok - one.q_off : -1;
+  if (a.n > 1) {
+    const AttnEntry mine = a.e[min(lane, a.n - 1)];
 #pragma unroll
-  for (int r = 0; r < 64 / TPR; ++r) {
-    const int t = __builtin_amdgcn_readlane(tok, r * TPR);
-    const uint64_t in = __ballot(lane < a.n && t >= mine.q_off && t < mine.q_off + mine.q_len);
-    const int pos = in ? __builtin_amdgcn_readlane(mine.prefix + t - mine.q_off, __builtin_ctzll(in)) : -1;
-    if (lane / TPR == r) qpos = pos;
+    for (int r = 0; r < 64 / TPR; ++r) {
+      const int t = __builtin_amdgcn_readlane(tok, r * TPR);
+      const uint64_t in = __ballot(lane < a.n && t >= mine.q_off && t < mine.q_off + mine.q_len);
+      const int pos = in ? __builtin_amdgcn_readlane(mine.prefix + t - mine.q_off, __builtin_ctzll(in)) : -1;
+      if (lane / TPR == r) qpos = pos;
+    }
   }
   if (row >= a.row_end || qpos < 0) return;        // a row of no entry of this launch
   const int ns = min(a.n_splits, qpos / a.split_len + 1);
