@@ -327,6 +327,61 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
   }
 }
 
+// Joins the splits of an int8 decode call: a wave for each query row.  Its partials, a
+// lane's four columns of every SPI-th split, are asked for at once, with the maxima and
+// sums (lane s: split s) and the entries, so the wave waits for memory once, where the
+// combine of the other pools, whose order of sums they keep, waits three to five times
+// (1331 keys in 21 splits 3.1 against 5.2 us, 40 ragged sequences 4.8 against 6.4).
+// Joining in the decode kernel itself, by the last wave of a sequence and KV head to
+// write, saves the launch and loses more: the partials then have to pass the caches of
+// the XCDs (32 x 8192 keys 103 us with device-scope accesses, 193 with fences, where the
+// two launches take 95 and 4.7; one sequence 17.4 against 10.4).
+// Splits past the row's own sequence hold older data and are left out.  A group of lanes
+// adds its splits in ascending order, then the groups are added: a fixed order.
+template <int D, int NI>
+__global__ void __launch_bounds__(256) join_splits_kernel(AttnArgs a, uint16_t* __restrict__ og) {
+  constexpr int LPR = D / 4, SPI = 64 / LPR;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = a.row_begin + blockIdx.x * (int)(blockDim.x >> 6) + w;
+  if (row >= a.row_end) return;
+  const int grp = lane / LPR, c0 = lane % LPR * 4;
+  const AttnEntry mine = a.e[min(lane, a.n - 1)];
+  const f32x2 ml = *(const f32x2*)(a.ws_ml + 2 * ((int64_t)min(lane, a.n_splits - 1) * a.n_rows + row));
+  f32x4 v[NI];
+#pragma unroll
+  for (int j = 0; j < NI; ++j)
+    v[j] = *(const f32x4*)(a.ws_acc + ((int64_t)min(j * SPI + grp, a.n_splits - 1) * a.n_rows + row) * D + c0);
+  const int tok = row / a.n_q_heads;
+  const uint64_t in = __ballot(lane < a.n && tok >= mine.q_off && tok < mine.q_off + mine.q_len);
+  if (in == 0) return;                             // a row of no entry of this launch
+  const int ns = __builtin_amdgcn_readlane((mine.prefix + mine.q_len - 1) / a.split_len + 1, __builtin_ctzll(in));
+  float M = lane < ns ? ml[0] : -INFINITY;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+  const float wgt = lane < ns ? __builtin_amdgcn_exp2f(ml[0] - M) : 0.f;
+  float L = lane < ns ? wgt * ml[1] : 0.f;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off);
+  f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < NI; ++j) {
+    const int s = j * SPI + grp;
+    const float ws = __shfl(wgt, s);               // s < 64
+    if (s < ns) o += ws * v[j];
+  }
+#pragma unroll
+  for (int off = LPR; off < 64; off <<= 1)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[q] += __shfl_xor(o[q], off);
+  if (grp == 0) *(bf16x4*)(og + (int64_t)row * D + c0) = __builtin_convertvector(o * (a.o_scale / L), bf16x4);
+}
+
+template <int D, int NI>
+void launch_join(const AttnArgs& a, hipStream_t s) {
+  const int rows = a.row_end - a.row_begin, per = rows >= 4096 ? 4 : 1;   // waves to a workgroup
+  hipLaunchKernelGGL((join_splits_kernel<D, NI>), dim3((rows + per - 1) / per), dim3(per * 64), 0, s, a, (uint16_t*)a.o);
+}
+
 template <int D, int B, int CK>
 void launch_dec(const AttnArgs& a, hipStream_t s) {
   using CT = cache_elem<CK>;
@@ -349,6 +404,22 @@ hipError_t launch_dec_d(const AttnArgs& a, hipStream_t s) {
 }  // namespace
 
 int attn_decode_keys_per_tile() { return kDecKT; }
+
+hipError_t launch_join_splits(const AttnArgs& a, hipStream_t s) {
+  if (a.row_begin < 0 || a.row_end > a.n_rows || a.n_splits > 64) return hipErrorInvalidValue;
+  if (a.row_end <= a.row_begin) return hipSuccess;
+  if (a.head_dim == 128) {
+    if (a.n_splits <= 8) launch_join<128, 4>(a, s);
+    else if (a.n_splits <= 24) launch_join<128, 12>(a, s);
+    else launch_join<128, 32>(a, s);
+  } else if (a.head_dim == 64) {
+    if (a.n_splits <= 24) launch_join<64, 6>(a, s);
+    else launch_join<64, 16>(a, s);
+  } else {
+    return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
 
 template <int CK>
 static hipError_t launch_dec_kind(const AttnArgs& a, hipStream_t s) {

@@ -298,6 +298,8 @@ hipError_t launch_attn_int8(const AttnArgs& a, hipStream_t s);
 // `cache`: kCacheBf16, kCacheFp8 or kCacheInt8 (attn_common.h).
 hipError_t launch_attn_decode(const AttnArgs& a, int cache, hipStream_t s);
 int attn_decode_keys_per_tile();
+// The combine of an int8 decode call (at most 64 splits): one round through memory.
+hipError_t launch_join_splits(const AttnArgs& a, hipStream_t s);
 // Merge split-key partials into O (bf16, or fp32 for fp32 pools), splits in
 // increasing order, `group` (8 or 16) of them to a round trip.
 hipError_t launch_split_combine(const AttnArgs& a, bool f32_out, int group, hipStream_t s);

@@ -642,7 +642,8 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
         a.n_tiles += (a.n_splits > 1 ? cdiv(kv[i], a.split_len) : 1) * p->hkv;
       }
       hipError_t err = launch_attn_decode(a, cache, st);
-      if (err == hipSuccess && a.n_splits > 1) err = launch_split_combine(a, false, 16, st);
+      if (err == hipSuccess && a.n_splits > 1)
+        err = cache == kCacheInt8 ? launch_join_splits(a, st) : launch_split_combine(a, false, 16, st);
       if (err != hipSuccess) return hip_fail(err, "decode attention launch");
       continue;
     }
