@@ -6,6 +6,7 @@ there is no fallback implementation.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 
@@ -170,6 +171,15 @@ def check(code: int) -> None:
         raise PgsrError(code, lib.pgsr_last_error().decode())
 
 
+def int32s(values) -> array.array:
+    """``values`` (anything that converts to int) as C ints."""
+    try:
+        return array.array("i", values)
+    except (TypeError, OverflowError):           # not integers, or past 32 bits: as ctypes converts them
+        whole = [int(v) for v in values]
+        return array.array("i", (ctypes.c_int32 * len(whole))(*whole))
+
+
 def int32_array(values):
-    values = [int(v) for v in values]
-    return (ctypes.c_int32 * max(1, len(values)))(*values)
+    a = values if isinstance(values, array.array) and values.typecode == "i" else int32s(values)
+    return (ctypes.c_int32 * len(a)).from_buffer(a) if len(a) else (ctypes.c_int32 * 1)()

@@ -179,10 +179,12 @@ class KVPool:
         dt, dv = self.dtype, self._dev
         if len(q_lens) != len(seqs):
             raise ValueError(f"{len(seqs)} sequences but {len(q_lens)} lengths")
-        if any(int(x) < 0 for x in q_lens):
+        lens = N.int32s(q_lens)
+        if lens and min(lens) < 0:
             raise ValueError("negative query length")
-        nq, nkv = prefill_sizes(self.hq, self.hkv, self.d, q_lens)
-        return fn(self._h, layer, len(seqs), N.int32_array(seqs), N.int32_array(q_lens),
+        tot = sum(lens)
+        nq, nkv = tot * self.hq * self.d, tot * self.hkv * self.d
+        return fn(self._h, layer, len(seqs), N.int32_array(seqs), N.int32_array(lens),
                   _dev_ptr(q, dt, "q", dv, nq), _dev_ptr(k, dt, "k", dv, nkv),
                   _dev_ptr(v, dt, "v", dv, nkv), _dev_ptr(o, dt, "o", dv, nq), float(scale),
                   N.COMMIT if commit else 0, ctypes.byref(self.recomputed_tokens),
