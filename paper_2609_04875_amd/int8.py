@@ -31,74 +31,80 @@ def _device(x: torch.Tensor, name: str) -> int:
 
 def _at(t: torch.Tensor, dtype: torch.dtype, name: str, dv: int, numel: int) -> Optional[int]:
     """``_dev_ptr`` with the checks that pass first: a re-decode step is as long as
-    its calls take on the host (10.7 against 13.1 us a call with three weights)."""
+    its calls take on the host."""
     if t.dtype is dtype and t.get_device() == dv and t.is_contiguous() and t.numel() == numel and numel:
         return t.data_ptr()
     return _dev_ptr(t, dtype, name, dv, numel)
 
 
-def _new(like: torch.Tensor, shape, dtype: torch.dtype, stream) -> torch.Tensor:
-    """A result of a call on ``stream`` (None: the current one), whose memory is that stream's."""
+def _result(t: Optional[torch.Tensor], like: torch.Tensor, shape, dtype: torch.dtype, name: str, dv: int, stream):
+    """A result of a call on ``stream`` (None: the current one) and its address:
+    the caller's tensor, checked, or a new one, whose memory is that stream's."""
+    if t is not None:
+        numel = 1
+        for n in shape:
+            numel *= n
+        return t, _at(t, dtype, name, dv, numel)
     if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
+        t = like.new_empty(shape, dtype=dtype)
+    else:
+        with torch.cuda.stream(stream):
+            t = like.new_empty(shape, dtype=dtype)
+    return t, t.data_ptr() or None
 
 
-def _rows(m: int, k: int, dv: int, like: torch.Tensor, out: Optional[torch.Tensor], scales: Optional[torch.Tensor],
-          stream):
-    """Codes [m, k] and scales [m] of a call, given or new, and their addresses."""
-    if out is None:
-        out = _new(like, (m, k), torch.int8, stream)
-    if scales is None:
-        scales = _new(like, (m,), torch.float32, stream)
-    return (out, scales), _at(out, torch.int8, "out", dv, m * k), _at(scales, torch.float32, "scales", dv, m)
+def _matrix(x: torch.Tensor, name: str):
+    if x.dim() != 2:
+        raise ValueError(f"{name} is {tuple(x.shape)}; it must be a matrix")
+    return x.shape
 
 
 def quantize_rows(x: torch.Tensor, out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                   stream=None) -> Rows:
     """Codes (int8 [m, k]) and scales (fp32 [m]) of the rows of ``x`` [m, k], bf16
     or fp32: scale = max |x| / 127, code = rint(x / scale)."""
-    if x.dim() != 2 or x.dtype not in _DT:
-        raise ValueError(f"x is {tuple(x.shape)} {x.dtype}; it must be [m, k], bf16 or fp32")
-    (m, k), dv = x.shape, _device(x, "x")
-    rows, qp, sp = _rows(m, k, dv, x, out, scales, stream)
+    (m, k), dv = _matrix(x, "x"), _device(x, "x")
+    if x.dtype not in _DT:
+        raise ValueError(f"x is {x.dtype}; it must be bf16 or fp32")
+    q, qp = _result(out, x, (m, k), torch.int8, "out", dv, stream)
+    s, sp = _result(scales, x, (m,), torch.float32, "scales", dv, stream)
     N.check(N.lib.pgsr_quantize_rows_int8(m, k, _DT[x.dtype], _at(x, x.dtype, "x", dv, m * k), qp, sp,
                                           _stream_ptr(stream, dv)))
-    return rows
+    return q, s
 
 
 def rmsnorm_int8(x: torch.Tensor, gain: torch.Tensor, eps: float, out: Optional[torch.Tensor] = None,
                  scales: Optional[torch.Tensor] = None, stream=None) -> Rows:
     """``quantize_rows`` of x / sqrt(mean(x^2) + eps) * gain (bf16 ``x`` [m, k],
     ``gain`` [k]), with no rounding in between."""
-    if x.dim() != 2:
-        raise ValueError(f"x is {tuple(x.shape)}; it must be [m, k]")
-    (m, k), dv = x.shape, _device(x, "x")
-    rows, qp, sp = _rows(m, k, dv, x, out, scales, stream)
+    (m, k), dv = _matrix(x, "x"), _device(x, "x")
+    q, qp = _result(out, x, (m, k), torch.int8, "out", dv, stream)
+    s, sp = _result(scales, x, (m,), torch.float32, "scales", dv, stream)
     N.check(N.lib.pgsr_rmsnorm_int8(m, k, _at(x, torch.bfloat16, "x", dv, m * k),
                                     _at(gain, torch.bfloat16, "gain", dv, k), eps, qp, sp, _stream_ptr(stream, dv)))
-    return rows
+    return q, s
 
 
 def silu_mul_int8(gate_up: torch.Tensor, out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                   stream=None) -> Rows:
     """``quantize_rows`` of SiLU(gate) * up for bf16 ``gate_up`` [m, 2 d_ff] (gate,
     then up), with no rounding in between."""
-    if gate_up.dim() != 2 or gate_up.shape[1] % 2:
+    (m, k2), dv = _matrix(gate_up, "gate_up"), _device(gate_up, "gate_up")
+    if k2 % 2:
         raise ValueError(f"gate_up is {tuple(gate_up.shape)}; it must be [m, 2 d_ff]")
-    (m, k), dv = (gate_up.shape[0], gate_up.shape[1] // 2), _device(gate_up, "gate_up")
-    rows, qp, sp = _rows(m, k, dv, gate_up, out, scales, stream)
-    N.check(N.lib.pgsr_silu_mul_int8(m, k, _at(gate_up, torch.bfloat16, "gate_up", dv, 2 * m * k), qp, sp,
+    k = k2 // 2
+    q, qp = _result(out, gate_up, (m, k), torch.int8, "out", dv, stream)
+    s, sp = _result(scales, gate_up, (m,), torch.float32, "scales", dv, stream)
+    N.check(N.lib.pgsr_silu_mul_int8(m, k, _at(gate_up, torch.bfloat16, "gate_up", dv, m * k2), qp, sp,
                                      _stream_ptr(stream, dv)))
-    return rows
+    return q, s
 
 
 def _weight(wq: torch.Tensor, ws: torch.Tensor, k: int, dv: int):
     """Rows of a weight, and the addresses of its codes and scales."""
-    if wq.dim() != 2 or wq.shape[1] != k:
+    n, k2 = _matrix(wq, "w")
+    if k2 != k:
         raise ValueError(f"w is {tuple(wq.shape)}; x has k = {k}")
-    n = wq.shape[0]
     return n, _at(wq, torch.int8, "w", dv, n * k), _at(ws, torch.float32, "ws", dv, n)
 
 
@@ -107,29 +113,28 @@ def gemm_int8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.Te
     """Y = (Xq Wq^T) * xs * ws (+ R), bf16: int8 codes ``xq`` [m, k], ``wq`` [n, k],
     fp32 scales of the tokens ``xs`` [m] and of the output channels ``ws`` [n]; the
     sums are exact.  ``r`` may be ``out``."""
-    if xq.dim() != 2:
-        raise ValueError(f"x is {tuple(xq.shape)}; it must be [m, k]")
-    (m, k), dv, bf = xq.shape, _device(xq, "x"), torch.bfloat16
+    (m, k), dv, bf = _matrix(xq, "x"), _device(xq, "x"), torch.bfloat16
     n, wp, wsp = _weight(wq, ws, k, dv)
-    if out is None:
-        out = _new(xq, (m, n), bf, stream)
+    y, yp = _result(out, xq, (m, n), bf, "out", dv, stream)
     N.check(N.lib.pgsr_gemm_int8(m, n, k, _at(xq, torch.int8, "x", dv, m * k), _at(xs, torch.float32, "xs", dv, m), wp, wsp,
-                                 _at(r, bf, "r", dv, m * n) if r is not None else None,
-                                 _at(out, bf, "out", dv, m * n), _stream_ptr(stream, dv)))
-    return out
+                                 _at(r, bf, "r", dv, m * n) if r is not None else None, yp, _stream_ptr(stream, dv)))
+    return y
 
 
 def gemm_int8_multi(xq: torch.Tensor, xs: torch.Tensor, wqs: Sequence[torch.Tensor], wss: Sequence[torch.Tensor],
                     outs: Sequence[torch.Tensor], stream=None) -> Sequence[torch.Tensor]:
     """out_i = (Xq Wq_i^T) * xs * ws_i for up to three weights: the bits of one
     ``gemm_int8`` each, in one launch."""
-    if xq.dim() != 2:
-        raise ValueError(f"x is {tuple(xq.shape)}; it must be [m, k]")
-    (m, k), dv, c = xq.shape, _device(xq, "x"), len(wqs)
+    (m, k), dv, c = _matrix(xq, "x"), _device(xq, "x"), len(wqs)
     if len(wss) != c or len(outs) != c:
         raise ValueError(f"{c} weights but {len(wss)} scales and {len(outs)} outputs")
-    ns, wps, wsps = zip(*[_weight(wq, ws, k, dv) for wq, ws in zip(wqs, wss)]) if c else ((), (), ())
-    yps = [_at(o, torch.bfloat16, "out", dv, m * n) for o, n in zip(outs, ns)]
+    ns, wps, wsps, yps = [], [], [], []
+    for wq, ws, out in zip(wqs, wss, outs):
+        n, wp, wsp = _weight(wq, ws, k, dv)
+        ns.append(n)
+        wps.append(wp)
+        wsps.append(wsp)
+        yps.append(_at(out, torch.bfloat16, "out", dv, m * n))
     ptrs = ctypes.c_void_p * c
     N.check(N.lib.pgsr_gemm_int8_multi(m, k, c, (ctypes.c_int32 * c)(*ns), _at(xq, torch.int8, "x", dv, m * k),
                                        _at(xs, torch.float32, "xs", dv, m), ptrs(*wps), ptrs(*wsps), ptrs(*yps),
