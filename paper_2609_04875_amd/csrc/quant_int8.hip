@@ -30,14 +30,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 enum Front { kRowsBf16, kRowsF32, kNorm, kGate };
 
 // SiLU(g) = g / (1 + e^-g) to about three roundings: e^-g = 2^t (1 + rest ln 2) with
-// t = -g log2(e) rounded and the rest kept, so a large |g| loses nothing; t past 126 is
-// cut (the result is below 2^-100 there).
+// t = -g log2(e) rounded and the rest kept, so a large |g| loses nothing; from t = 126
+// on, where e^-g leaves fp32, it is 0 (below 2^-119; -inf gives NaN).
 __device__ inline float silu_fast(float g) {
   constexpr float kL = 1.44269504f, kLLo = 1.92596299e-8f;   // log2(e) = kL + kLLo
-  const float t = fminf(g * -kL, 126.f);
+  const float t = g * -kL;
   const float rest = fmaf(g, -kLLo, fmaf(g, -kL, -t));
   const float e = __builtin_amdgcn_exp2f(t);
-  return g * __builtin_amdgcn_rcpf(1.f + fmaf(e, t < 126.f ? rest * 0.69314718f : 0.f, e));
+  const float r = __builtin_amdgcn_rcpf(1.f + fmaf(e, rest * 0.69314718f, e));
+  return g * (t < 126.f ? r : 0.f);
 }
 
 // Eight values of a row from column c; NORM: x * gain, still without the factor of

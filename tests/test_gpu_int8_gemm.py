@@ -102,6 +102,23 @@ def test_rows_that_are_not_finite():
     assert torch.isfinite(y[0]).all() and torch.isnan(y[1:]).all()
 
 
+def test_gates_far_from_zero():
+    """SiLU of gates from the smallest to the largest: 0 far below, the gate itself
+    far above; a row of far negative gates is a row of zeros."""
+    g = torch.tensor([-3e38, -1e30, -1000.0, -126.0, -88.0, -87.0, -60.0, -20.0, -1e-30, 0.0, 1e-30, 20.0, 90.0, 1000.0,
+                      -0.0, 3e-39], dtype=torch.float64)
+    for gate in (g, g.clamp(max=-90.0), g.clamp(max=-50.0), g.clamp(max=1.0), g.clamp(max=1e-30)):
+        gu = torch.cat([gate, torch.ones(16, dtype=torch.float64)])[None].to(BF).cuda()
+        q, s = silu_mul_int8(gu)
+        y = Q.silu_mul(np.maximum(_np(gu), -700.0))
+        y[np.abs(y) < 2.0 ** -119] = 0                  # below what the kernel keeps
+        top = np.abs(y).max()
+        if top == 0:
+            assert s.item() == 0 and not q.any()
+        else:
+            _check_codes(q.cpu().numpy(), s.cpu().numpy().astype(np.float64), y, 40)
+
+
 def test_more_rows_than_one_launch():
     m = (1 << 21) + 3
     x = torch.ones(m, 16, dtype=BF, device="cuda")
