@@ -409,6 +409,66 @@ def test_static_scratch_equals_the_workspace():
         assert torch.equal(oa, ob)
 
 
+def test_caches_past_32_bits():
+    """Blocks at the end of a cache of more than 2^32 codes: prefill (four-wave,
+    pipelined, through the copy) and decode as in a small pool."""
+    from paper_2609_04875_amd import INT8, KVPool
+    geom, n_blocks = W.AttnGeometry(32, 8, 128), 270000
+    log(f"int8 cache of {n_blocks * 16384:.2e} codes")
+    rng = np.random.default_rng(61)
+    order = list(range(n_blocks))                                # pops yield the last ids first
+    far = KVPool(1, 32, 8, 128, n_blocks, 1, 256, INT8, 16, order, workspace_bytes=64 << 20)
+    near = KVPool(1, 32, 8, 128, 256, 1, 256, INT8, 16, workspace_bytes=64 << 20)
+    a = [_bf16(_rand(rng, 45, h, 128)) for h in (32, 8, 8)]
+    b = [_bf16(_rand(rng, 2070, h, 128)) for h in (32, 8, 8)]
+    c = [_bf16(_rand(rng, 1, h, 128)) for h in (32, 8, 8)]
+    outs = []
+    for pool in (far, near):
+        for kernel in ("four_wave", "pipelined", "auto"):
+            pool.set_prefill_kernel(kernel)
+            if pool.seq_len(0):
+                assert pool.crop([0], [0]) == 0
+            for x in (a, b, c):
+                outs.append(torch.empty_like(x[0]))
+                assert pool.replay(0, [0], [len(x[0])], *x, outs[-1], 0.09) == 0
+    assert int(far.block_tables[0, :120].min()) > 262144          # past 2^32 bytes of codes
+    assert all(torch.equal(x, y) for x, y in zip(outs[:9], outs[9:]))
+
+
+def test_captured_prefill_through_the_copy():
+    """A long suffix recorded with its copy in the workspace, replayed with other
+    inputs and eager calls that use the same workspace in between."""
+    geom = W.AttnGeometry(8, 2, 128)
+    rng = np.random.default_rng(71)
+    pool = _pool(geom, 300, 1, 300, split_q=200, max_splits=16)
+    z = [_bf16(_rand(rng, 700, h, 128)) for h in (8, 2, 2)]
+    assert pool.replay(0, [0], [700], *z, torch.empty_like(z[0]), 0.09) == 0
+    n = 64 * 140
+    pool2 = _pool(geom, 700, 1, 700, split_q=n, max_splits=2)
+    assert pool2.replay(0, [0], [700], *z, torch.empty_like(z[0]), 0.09) == 0
+    xs = [[torch.randn(n, h, 128, device="cuda").to(torch.bfloat16) for h in (8, 2, 2)] for _ in range(3)]
+    want = []
+    for x in xs:
+        want.append(torch.empty_like(x[0]))
+        pool2.workspace.fill_(0xA5)
+        assert pool2.replay(0, [0], [n], *x, want[-1], 0.09, commit=False) == 0
+        torch.cuda.synchronize()
+        assert (pool2.workspace[:4096] != 0xA5).any()                # the copy was made
+    held, out = [t.clone() for t in xs[0]], torch.empty_like(want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        assert pool2.replay(0, [0], [n], *held, out, 0.09, commit=False) == 0
+    for i in (0, 2, 1, 0):
+        for p, q in zip(held, xs[i]):
+            p.copy_(q)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i])
+        one = [t[:1].clone() for t in xs[1]]
+        assert pool2.replay(0, [0], [1], *one, torch.empty_like(one[0]), 0.09, commit=False) == 0
+        torch.cuda.synchronize()
+
+
 def test_refusals_change_nothing():
     import ctypes
     from paper_2609_04875_amd import BF16, EINVAL, INT8, KVPool

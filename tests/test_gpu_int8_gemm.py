@@ -119,6 +119,39 @@ def test_gates_far_from_zero():
             _check_codes(q.cpu().numpy(), s.cpu().numpy().astype(np.float64), y, 40)
 
 
+def test_sizes_past_32_bits():
+    """x, w and y each of more than 2^31 elements, their last rows and columns against
+    products of those alone."""
+    log("x of 2.3e9 codes")
+    m, k, n = 140008, 16400, 8
+    x = torch.zeros(m, k, dtype=torch.int8, device="cuda")
+    part = torch.randint(-127, 128, (300, k), dtype=torch.int8, device="cuda")
+    x[-300:] = part
+    s, ws = torch.rand(m, device="cuda") + 0.5, torch.rand(n, device="cuda") + 0.5
+    w = torch.randint(-127, 128, (n, k), dtype=torch.int8, device="cuda")
+    y = gemm_int8(x, s, w, ws)
+    assert torch.equal(y[-300:], gemm_int8(part, s[-300:].clone(), w, ws)) and not y[:-300].any()
+    log("w of 2.3e9 codes")
+    y = gemm_int8(w[:3].contiguous(), s[:3].contiguous(), x, s)
+    assert torch.equal(y[:, -304:], gemm_int8(w[:3].contiguous(), s[:3].contiguous(), x[-304:], s[-304:].clone()))
+    assert not y[:, :-304].any()
+    del x, y
+    log("rows of 2.3e9 values")
+    x = torch.zeros(m, k, dtype=BF, device="cuda")
+    x[-2:] = torch.randn(2, k, device="cuda").to(BF)
+    q, sc = quantize_rows(x)
+    q2, s2 = quantize_rows(x[-2:].contiguous())
+    assert torch.equal(q[-2:], q2) and torch.equal(sc[-2:], s2) and not q[-9:-2].any() and not sc[:-2].any()
+    del x, q
+    log("y of 4.4e9 values")
+    m = n = 66000
+    x, w = torch.zeros(m, 16, dtype=torch.int8, device="cuda"), torch.zeros(n, 16, dtype=torch.int8, device="cuda")
+    x[-5:], w[-9:] = 3, 2
+    one = torch.ones(m, device="cuda")
+    y = gemm_int8(x, one, w, one)
+    assert (y[-5:, -9:] == 96).all() and not y[-5:, :-9].any() and not y[-6].any() and not y[0].any()
+
+
 def test_more_rows_than_one_launch():
     m = (1 << 21) + 3
     x = torch.ones(m, 16, dtype=BF, device="cuda")
