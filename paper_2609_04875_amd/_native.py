@@ -171,15 +171,17 @@ def check(code: int) -> None:
         raise PgsrError(code, lib.pgsr_last_error().decode())
 
 
-def int32s(values) -> array.array:
-    """``values`` (anything that converts to int) as C ints."""
+def int32s(values):
+    """``values`` (anything that converts to int) as C ints; a list of ints where one
+    of them does not fit or is no integer."""
     try:
-        return array.array("i", values)
-    except (TypeError, OverflowError):           # not integers, or past 32 bits: as ctypes converts them
-        whole = [int(v) for v in values]
-        return array.array("i", (ctypes.c_int32 * len(whole))(*whole))
+        return array.array("i", iter(values))
+    except (TypeError, OverflowError):
+        return [int(v) for v in values]
 
 
 def int32_array(values):
     a = values if isinstance(values, array.array) and values.typecode == "i" else int32s(values)
-    return (ctypes.c_int32 * len(a)).from_buffer(a) if len(a) else (ctypes.c_int32 * 1)()
+    if len(a) == 0 or isinstance(a, list):
+        return (ctypes.c_int32 * max(1, len(a)))(*a)
+    return (ctypes.c_int32 * len(a)).from_buffer(a)

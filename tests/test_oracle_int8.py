@@ -79,3 +79,25 @@ def test_exponents_are_refused_without_a_pool():
         a = {"hq": 32, "hkv": 8, "d": 128, "B": 16, "nb": 64, **bad}
         assert N.lib.pgsr_pool_create(1, a["hq"], a["hkv"], a["d"], a["B"], N.INT8, a["nb"], 2, 8, fake, fake, fake,
                                       fake, fake, fake, fake, None, 0, None, None, ctypes.byref(out)) == code
+
+
+def test_lists_of_a_call_convert_as_ints(monkeypatch):
+    """Sequence ids and lengths of any integer-like type, and a length past 32 bits,
+    which must not pass for the one its low bits name."""
+    import types
+
+    import torch
+    from paper_2609_04875_amd import _native as N, pool as P
+    for values in ([3, 1], (3, 1), b"\x03\x01", np.array([3, 1]), np.array([3, 1], np.int32), torch.tensor([3, 1]),
+                   [3.0, 1.0], [np.int64(3), True], range(3, 0, -2), N.int32s([3, 1])):
+        assert list(N.int32_array(values)) == [3, 1], values
+    assert list(N.int32_array([])) == [0]
+    seen = []
+    pool = types.SimpleNamespace(_h=None, dtype=torch.bfloat16, _dev=0, hq=8, hkv=2, d=64,
+                                 recomputed_tokens=ctypes.c_int64(0))
+    monkeypatch.setattr(P, "_dev_ptr", lambda t, dt, name, dv, numel: seen.append((name, numel)))
+    monkeypatch.setattr(P, "_stream_ptr", lambda stream, dv=None: None)
+    P.KVPool._prefill(pool, lambda *a: 0, 0, [0], [2 ** 32 + 3], None, None, None, None, 1.0, True, None)
+    assert seen[0] == ("q", (2 ** 32 + 3) * 8 * 64) and seen[1] == ("k", (2 ** 32 + 3) * 2 * 64)
+    with pytest.raises(ValueError):
+        P.KVPool._prefill(pool, lambda *a: 0, 0, [0, 1], [1, -2 ** 40], None, None, None, None, 1.0, True, None)
