@@ -290,7 +290,8 @@ int pgsr_full_reset_prefill(pgsr_pool *pool, int32_t layer, int32_t n, const int
  * call records HIP events on its stream around its append launches and around
  * its attention launches (a few microseconds of overhead per call).
  * pgsr_pool_last_times waits for the most recent such call's events and
- * returns the GPU time of its append and attention kernels in milliseconds.
+ * returns the GPU time of its append and attention kernels in milliseconds (an
+ * int8 pool with a workspace appends single tokens in its attention kernel).
  */
 int pgsr_pool_enable_timing(pgsr_pool *pool, int on);
 int pgsr_pool_last_times(pgsr_pool *pool, float *append_ms, float *attention_ms);

@@ -34,14 +34,19 @@
 // slots never reach the result.  The online softmax (base 2, lazy rescale,
 // row sum of the bf16-rounded P) is the prefill kernel's.  With several
 // splits a wave writes unnormalised partials (m, l, acc) of its split and the
-// split combine merges them in increasing split order; with one split it
-// writes O.
+// split combine (int8: join_splits_kernel) merges them in a fixed order; with one
+// split it writes O.
+//
+// Int8 codes go into the products as they are (bf16 holds integers to 256): S is
+// scaled by the powers of two of its keys and P by those of V's keys, 32 products a
+// lane and tile where scaling the operands would take one for each of its codes.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 #include <type_traits>
 
 #include "attn_common.h"
+#include "int8_rows.h"
 #include "internal.h"
 
 namespace pgsr {
@@ -51,11 +56,23 @@ namespace {
 constexpr int kDecKT = 32;          // keys per tile
 constexpr float kDecSlack = 8.f;    // lazy rescale threshold, log2 units
 
+struct NoAppend {};
+template <int CK>
+using NewTokens = std::conditional_t<CK == kCacheInt8, DecodeAppend, NoAppend>;
+
+// Byte i (of 16, the same in every lane) of w.
+__device__ inline void set_byte(u32x4& w, int i, uint32_t byte, bool mine) {
+  const int sh = 8 * (i & 3);
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    if (mine && q == i / 4) w[q] = (w[q] & ~(0xFFu << sh)) | (byte << sh);
+}
+
 template <int D, int B, int CK>
 __global__ void __launch_bounds__(256, 2)
 attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_t* __restrict__ qg_,
                    const cache_elem<CK>* __restrict__ kc, const cache_elem<CK>* __restrict__ vc,
-                   uint16_t* __restrict__ og) {
+                   uint16_t* __restrict__ og, NewTokens<CK> f) {
   constexpr int KT = kDecKT;
   constexpr bool kByte = CK != kCacheBf16;       // one-byte codes
   constexpr bool I8 = CK == kCacheInt8;
@@ -92,6 +109,31 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
   const int key_lo = a.n_splits > 1 ? split * a.split_len : 0;
   const int key_hi = a.n_splits > 1 ? min(kv_len, key_lo + a.split_len) : kv_len;
 
+  // Int8: this wave's split ends with a token that is not in the cache yet (one token
+  // to a sequence, so no other wave of the KV head reads its place).  Lanes below C
+  // take its K row, 8 values each, and the next C its V row; the codes go into the
+  // last tile's operands in registers and, behind the loop, into the cache.  Against an
+  // append launch before this one: one sequence of 1331 keys 15.6 -> 11.5 us a call, 32
+  // of 8192 104 -> 100.4 (the launch 5.2 us, this kernel 2 to 3 more).  The tile is
+  // patched where its loads are waited for in any case: ahead of that, or with the
+  // new tokens' blocks picked by a select, the loop waits for all loads (4 us more).
+  constexpr int C = D / 8;
+  bool fresh = false;
+  int32_t new_id = -1;                             // its block, where it is a new one
+  int32_t last = kv_len - 1;                       // last key whose place is read
+  u32x4 raw_kv{};
+  if constexpr (I8) {
+    fresh = f.k_in != nullptr && split == ns - 1;
+    if (fresh) {
+      raw_kv = *(const u32x4*)((const uint16_t*)(lane % (2 * C) < C ? f.k_in : f.v_in) +
+                               ((int64_t)e.q_off * hkv + g) * D + lane % C * 8);
+      if (f.pop[ei] >= 0) {
+        new_id = blk_id(f.free_list[f.pop[ei]], a.n_blocks, a.chk);
+        last = max(e.prefix - 1, 0);               // the table does not hold the new block yet
+      }
+    }
+  }
+
   // Q^T operand: lane (row r, half hh) holds d in [hh D/2 + 8 ds, +8).
   bf16x8 qb[kQLds ? 1 : NDS];
   uint16_t* const q_mine = &q_lds[kQLds ? ((threadIdx.x >> 6) * 32 + r) * QLD + hh * (D / 2) : 0];
@@ -114,10 +156,10 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
   const int32_t* __restrict__ row = tables + (int64_t)e.seq * a.max_bps;
   const int64_t head_base = (int64_t)a.layer * a.n_blocks * hkv + g;   // + id * hkv
   const int kperm = 16 * ((r >> 2) & 1) + 4 * (r >> 3) + (r & 3);     // key of K operand row r
-  auto k_key = [&](int kb) { return min(kb + kperm, kv_len - 1); };
+  auto k_key = [&](int kb) { return min(kb + kperm, last); };
   auto v_key = [&](int kb) {                                           // first of this lane's 16 V keys
     const int k0 = kb + 16 * hh;
-    return k0 < kv_len ? k0 : ((kv_len - 1) & ~15);
+    return k0 <= last ? k0 : (last & ~15);
   };
   auto k_id = [&](int kb) { return blk_id(row[k_key(kb) / B], a.n_blocks, a.chk); };
   auto v_id = [&](int kb) { return blk_id(row[v_key(kb) / B], a.n_blocks, a.chk); };
@@ -194,13 +236,38 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
   // 6% for bf16 and ties for FP8: fewer bytes in flight per CU keep the HBM
   // queues shorter.
   const int n_kt = (key_hi - key_lo + KT - 1) / KT;
-  load_k(key_lo, k_id(key_lo));
-  load_v(key_lo, v_id(key_lo));
-  load_e(key_lo, v_id(key_lo));
+  int idk0, idv0;
+  if (I8 && new_id >= 0 && e.prefix == 0) {        // the only token: there is no block in the table
+    idk0 = idv0 = new_id;
+  } else {
+    idk0 = k_id(key_lo);
+    idv0 = v_id(key_lo);
+  }
+  load_k(key_lo, idk0);
+  load_v(key_lo, idv0);
+  load_e(key_lo, idv0);
   int idk_n = 0, idv_n = 0;
   if (n_kt > 1) {
     idk_n = k_id(key_lo + KT);
     idv_n = v_id(key_lo + KT);
+  }
+  u32x2 codes{};                                   // of the new token: 8 values of K or V a lane
+  uint32_t exps = 0;                               // its exponent bytes, K's and (8 bits up) V's
+  if constexpr (I8) {
+    if (fresh) {
+      uint16_t x[8];
+      halves(raw_kv, x);
+      RowMax mine;
+      row_max(x, mine);
+      int nan;
+      const uint32_t top = rows_max<C>(mine, RowMax{}, nan);
+      nan |= __shfl_xor(nan, C);                   // K's and V's
+      const bool is_k = lane % (2 * C) < C;
+      const int own = row_exp(top & 0xFFFFu);
+      codes = codes8(x, own, is_k && nan);
+      const int ke1 = __builtin_amdgcn_readlane(own, 0), ve1 = __builtin_amdgcn_readlane(own, C);
+      exps = (__builtin_amdgcn_readlane(nan, 0) ? 255u : (uint32_t)(ke1 + 127)) | ((uint32_t)(ve1 + 127) << 8);
+    }
   }
   for (int j = 0; j < n_kt; ++j) {
     const int kb = key_lo + j * KT;
@@ -208,7 +275,23 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
     u32x4 kcur[NK], vcur[NV];
 #pragma unroll
     for (int c = 0; c < NK; ++c) kcur[c] = kr[c];
-    if (more) load_k(kb + KT, idk_n);
+    if (more) {
+      load_k(kb + KT, idk_n);
+    } else if constexpr (I8) {
+      if (fresh) {                                 // the new token's codes and exponents in its place
+        const int t0 = e.prefix - kb;
+        set_byte(ke, t0 & 15, exps & 0xFFu, hh == t0 >> 4);
+        set_byte(ve, t0 & 15, exps >> 8, hh == t0 >> 4);
+#pragma unroll
+        for (int c = 0; c < NK; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = __builtin_amdgcn_readlane(codes[i % 2], 2 * c + i / 2);
+            const uint32_t hi = __builtin_amdgcn_readlane(codes[i % 2], D / 16 + 2 * c + i / 2);
+            if (kperm == t0) kcur[c][i] = hh ? hi : lo;
+          }
+      }
+    }
     f32x16 s = f32x16{};
 #pragma unroll
     for (int ds = 0; ds < NDS; ++ds)
@@ -233,6 +316,16 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
       if (j + 2 < n_kt) {
         idk_n = k_id(kb + 2 * KT);
         idv_n = v_id(kb + 2 * KT);
+      }
+    } else if constexpr (I8) {
+      if (fresh) {
+        const int t0 = e.prefix - kb;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          const int from = C + (r + 32 * db) / 8;
+          const uint32_t w0 = __shfl(codes[0], from), w1 = __shfl(codes[1], from);
+          set_byte(vcur[db], t0 & 15, ((r & 4 ? w1 : w0) >> (8 * (r & 3))) & 0xFFu, hh == t0 >> 4);
+        }
       }
     }
     // lane half hh holds keys kb + 16 hh + v; mask those past the row's position
@@ -300,6 +393,28 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
       }
   }
 
+  if constexpr (I8) {
+    if (fresh) {                                   // the append itself, as append_int8_kernel's
+      const int32_t id = new_id >= 0 ? new_id : blk_id(row[e.prefix / B], a.n_blocks, a.chk);
+      const int slot = e.prefix % B;
+      const int64_t head = head_base + (int64_t)id * hkv;
+      if (lane < C) *(u32x2*)((uint8_t*)kc + (head * B + slot) * D + lane * 8) = codes;
+      if (lane >= C && lane < 2 * C) {
+        uint8_t* vp = (uint8_t*)vc + (head * D + (lane - C) * 8) * B + slot;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) vp[i * B] = (uint8_t)(codes[i / 4] >> (8 * (i % 4)));
+      }
+      if (lane < 2) f.kv_exps[(head * 2 + lane) * B + slot] = (uint8_t)(exps >> (8 * lane));
+      if (g == 0 && lane == 0) {
+        if (new_id >= 0) {
+          ((int32_t*)row)[e.prefix / B] = new_id;
+          f.refs[new_id] = 1;
+        }
+        if (f.commit) f.lens[e.seq] = e.prefix + 1;
+      }
+    }
+    if (f.k_in != nullptr && wid == 0 && lane == 0) *f.free_top = f.top_after;
+  }
   const float l_tot = l + xor32(l);
   if (!valid) return;
   const int64_t qrow = (int64_t)(e.q_off + tok) * a.n_q_heads + hq;
@@ -383,19 +498,19 @@ void launch_join(const AttnArgs& a, hipStream_t s) {
 }
 
 template <int D, int B, int CK>
-void launch_dec(const AttnArgs& a, hipStream_t s) {
+void launch_dec(const AttnArgs& a, const NewTokens<CK>& f, hipStream_t s) {
   using CT = cache_elem<CK>;
   hipLaunchKernelGGL((attn_decode_kernel<D, B, CK>), dim3((unsigned)((a.n_tiles + 3) / 4)), dim3(256), 0, s, a,
                      a.tables, (const uint16_t*)a.q, (const CT*)a.k_cache, (const CT*)a.v_cache,
-                     (uint16_t*)a.o);
+                     (uint16_t*)a.o, f);
 }
 
 template <int D, int CK>
-hipError_t launch_dec_d(const AttnArgs& a, hipStream_t s) {
+hipError_t launch_dec_d(const AttnArgs& a, const NewTokens<CK>& f, hipStream_t s) {
   switch (a.block_size) {
-    case 16: launch_dec<D, 16, CK>(a, s); break;
-    case 32: launch_dec<D, 32, CK>(a, s); break;
-    case 64: launch_dec<D, 64, CK>(a, s); break;
+    case 16: launch_dec<D, 16, CK>(a, f, s); break;
+    case 32: launch_dec<D, 32, CK>(a, f, s); break;
+    case 64: launch_dec<D, 64, CK>(a, f, s); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
@@ -422,17 +537,16 @@ hipError_t launch_join_splits(const AttnArgs& a, hipStream_t s) {
 }
 
 template <int CK>
-static hipError_t launch_dec_kind(const AttnArgs& a, hipStream_t s) {
-  if (a.head_dim == 128) return launch_dec_d<128, CK>(a, s);
-  if (a.head_dim == 64) return launch_dec_d<64, CK>(a, s);
+static hipError_t launch_dec_kind(const AttnArgs& a, const NewTokens<CK>& f, hipStream_t s) {
+  if (a.head_dim == 128) return launch_dec_d<128, CK>(a, f, s);
+  if (a.head_dim == 64) return launch_dec_d<64, CK>(a, f, s);
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_attn_decode(const AttnArgs& a, int cache, hipStream_t s) {
+hipError_t launch_attn_decode(const AttnArgs& a, int cache, const DecodeAppend& f, hipStream_t s) {
   if (a.n <= 0) return hipSuccess;
-  return cache == kCacheFp8    ? launch_dec_kind<kCacheFp8>(a, s)
-         : cache == kCacheInt8 ? launch_dec_kind<kCacheInt8>(a, s)
-                               : launch_dec_kind<kCacheBf16>(a, s);
+  if (cache == kCacheInt8) return launch_dec_kind<kCacheInt8>(a, f, s);
+  return cache == kCacheFp8 ? launch_dec_kind<kCacheFp8>(a, {}, s) : launch_dec_kind<kCacheBf16>(a, {}, s);
 }
 
 }  // namespace pgsr

@@ -292,11 +292,26 @@ hipError_t launch_attn_bf16_narrow(const AttnArgs& a, int waves, hipStream_t s);
 hipError_t launch_attn_fp8(const AttnArgs& a, hipStream_t s);
 // And over an int8 cache: each code times its token's power of two is a bf16 value.
 hipError_t launch_attn_int8(const AttnArgs& a, hipStream_t s);
+// What a decode launch of an int8 pool does for an append: one new token to a
+// sequence, quantised by the wave whose split ends with it (k_in null: the call's
+// tokens are in the cache).
+struct DecodeAppend {
+  const void* k_in;
+  const void* v_in;
+  int32_t* lens;
+  const int32_t* free_list;
+  int32_t* free_top;
+  int32_t* refs;
+  uint8_t* kv_exps;
+  int32_t commit;
+  int32_t top_after;
+  int32_t pop[kMaxSeqsPerLaunch];   // place in free_list of the entry's new block, -1: it has one
+};
 // Decode attention (every sequence of the launch has at most 32 / G query
 // tokens): one wave per (sequence, KV head, split) gathering MFMA operands from
 // the cache without LDS; with n_splits > 1 it writes split partials.
 // `cache`: kCacheBf16, kCacheFp8 or kCacheInt8 (attn_common.h).
-hipError_t launch_attn_decode(const AttnArgs& a, int cache, hipStream_t s);
+hipError_t launch_attn_decode(const AttnArgs& a, int cache, const DecodeAppend& f, hipStream_t s);
 int attn_decode_keys_per_tile();
 // The combine of an int8 decode call (at most 64 splits): one round through memory.
 hipError_t launch_join_splits(const AttnArgs& a, hipStream_t s);

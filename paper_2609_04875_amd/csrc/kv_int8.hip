@@ -27,6 +27,7 @@
 #include <hip/hip_runtime.h>
 
 #include "attn_common.h"
+#include "int8_rows.h"
 #include "internal.h"
 
 namespace pgsr {
@@ -34,41 +35,6 @@ namespace pgsr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kExpLo = -100, kExpHi = 100;
-
-// What eight values of a row give: the largest magnitude's bits, and whether one is NaN.
-struct RowMax {
-  uint32_t bits = 0;      // of |x|, an integer order
-  bool nan = false;
-};
-
-__device__ inline void row_max(const uint16_t (&x)[8], RowMax& m) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t b = x[j] & 0x7FFFu;
-    if (b > 0x7F80u) m.nan = true;
-    else m.bits = max(m.bits, b);
-  }
-}
-
-// e of a row whose largest magnitude has these bf16 bits
-__device__ inline int row_exp(uint32_t bits) {
-  return min(max((int)(bits >> 7) - 127 - 6, kExpLo), kExpHi);   // zeros and subnormals: the lowest
-}
-
-// Eight codes of x 2^-e, in element order.
-__device__ inline u32x2 codes8(const uint16_t (&x)[8], int e, bool none) {
-  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-  u32x2 r = {0, 0};
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float f = __uint_as_float((uint32_t)x[j] << 16) * inv;
-    const float c = fminf(fmaxf(__builtin_rintf(f), -127.f), 127.f);
-    const int code = none || f != f ? 0 : (int)c;
-    r[j / 4] |= (uint32_t)(uint8_t)code << (8 * (j % 4));
-  }
-  return r;
-}
 
 // Block ids, table, counts, lengths and stack top as append_kernel (kv_pool.hip)
 // writes them; the copies are the quantisation above.
@@ -118,12 +84,8 @@ __global__ void __launch_bounds__(kThreads) append_int8_kernel(AppendArgs a) {
     if (t < nt) {
       const uint16_t *kp = kin + t * row_stride + c, *vp = vin + t * row_stride + c;
       if (wide) {
-        const u32x4 kw = *(const u32x4*)kp, vw = *(const u32x4*)vp;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          kx[j] = (uint16_t)(kw[j / 2] >> (16 * (j % 2)));
-          vx[j] = (uint16_t)(vw[j / 2] >> (16 * (j % 2)));
-        }
+        halves(*(const u32x4*)kp, kx);
+        halves(*(const u32x4*)vp, vx);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -135,16 +97,8 @@ __global__ void __launch_bounds__(kThreads) append_int8_kernel(AppendArgs a) {
     RowMax mk, mv;
     row_max(kx, mk);
     row_max(vx, mv);
-    // both maxima and the flag through one word and one shuffle a step: magnitudes
-    // have 15 bits
-    uint32_t packed = mk.bits | (mv.bits << 16);
-    int nan = mk.nan || mv.nan;
-#pragma unroll
-    for (int off = C / 2; off >= 1; off >>= 1) {
-      const uint32_t o = __shfl_xor(packed, off);
-      packed = max(packed & 0xFFFFu, o & 0xFFFFu) | (max(packed >> 16, o >> 16) << 16);
-      nan |= __shfl_xor(nan, off);
-    }
+    int nan;
+    const uint32_t packed = rows_max<C>(mk, mv, nan);
     if (t < nt) {
       const int ke = row_exp(packed & 0xFFFFu), ve = row_exp(packed >> 16);
       *(u32x2*)(kc + (s0 + t) * D + c) = codes8(kx, ke, nan != 0);

@@ -240,8 +240,11 @@ int do_crop(pgsr_pool* p, int32_t n, const int32_t* seqs, const int32_t* new_len
 }
 
 // ---------------------------------------------------------------- replay -- //
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
 struct Seg {
   int32_t seq, prefix, q_len, q_off;
+  int32_t pop = -1;        // appends of a decode launch: place in the free stack of a new block
 };
 
 constexpr int64_t kCus = 256;
@@ -420,6 +423,16 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
   }
   const bool commit = (flags & PGSR_COMMIT) != 0;
   const int eb = elem_bytes(p);
+  const int group = p->hq / p->hkv;
+  // Decode path: every sequence's queries fit one wave (32 / G tokens) and the
+  // pool has a workspace (so batching already decides the rounding order).
+  bool decode = p->dtype != PGSR_F32 && ws_bytes > 0;
+  for (const Seg& g : segs) decode = decode && g.q_len <= 32 / group;
+  // Int8, one new token to each sequence and no shared tail to copy: the decode kernel
+  // appends it itself.
+  bool append_in_decode = decode && p->dtype == PGSR_INT8 && aligned16(k) && aligned16(v);
+  for (const Seg& g : segs)
+    append_in_decode = append_in_decode && g.q_len == 1 && !shared_tail(p, g.seq, g.prefix, g.q_len);
 
   if (p->timing) {
     hipError_t err = hipEventRecord(p->ev[0], st);
@@ -534,8 +547,10 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
         p->h_ref[nb] = 1;
         row[lb] = nb;
       }
+      if (end_blocks > p->h_nalloc[g.seq]) segs[base + i].pop = e.stack_before - 1;
       p->h_nalloc[g.seq] = std::max(p->h_nalloc[g.seq], end_blocks);
     }
+    if (append_in_decode) continue;
     a.n_items = items;
     a.write_top = 1;
     a.top_after = p->h_top;
@@ -550,11 +565,6 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
     if (err != hipSuccess) return hip_fail(err, "timing event");
   }
   // Attention, chunked; within a launch, costlier sequences first.
-  const int group = p->hq / p->hkv;
-  // Decode path: every sequence's queries fit one wave (32 / G tokens) and the
-  // pool has a workspace (so batching already decides the rounding order).
-  bool decode = p->dtype != PGSR_F32 && ws_bytes > 0;
-  for (const Seg& g : segs) decode = decode && g.q_len <= 32 / group;
   int64_t max_kv = 0;
   for (const Seg& g : segs) max_kv = std::max<int64_t>(max_kv, (int64_t)g.prefix + g.q_len);
   // Kernels of one arithmetic (the same bits for every row of one split plan).  The
@@ -641,7 +651,20 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
         a.e[i].tile_start = a.n_tiles;
         a.n_tiles += (a.n_splits > 1 ? cdiv(kv[i], a.split_len) : 1) * p->hkv;
       }
-      hipError_t err = launch_attn_decode(a, cache, st);
+      DecodeAppend f{};
+      if (append_in_decode) {
+        f.k_in = k;
+        f.v_in = v;
+        f.lens = p->lens;
+        f.free_list = p->free_list;
+        f.free_top = p->free_top;
+        f.refs = p->refs;
+        f.kv_exps = p->kv_exps;
+        f.commit = commit ? 1 : 0;
+        f.top_after = p->h_top;
+        for (int32_t i = 0; i < cnt; ++i) f.pop[i] = chunk[i].pop;
+      }
+      hipError_t err = launch_attn_decode(a, cache, f, st);
       if (err == hipSuccess && a.n_splits > 1)
         err = cache == kCacheInt8 ? launch_join_splits(a, st) : launch_split_combine(a, false, 16, st);
       if (err != hipSuccess) return hip_fail(err, "decode attention launch");
@@ -1268,7 +1291,6 @@ int pgsr_gemm_bf16(int32_t m, int32_t n, int32_t k, const void* x, const void* w
   return ok();
 }
 
-static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 int pgsr_gemm_bf16_multi(int32_t m, int32_t k, int32_t count, const int32_t* n, const void* x,
                          const void* const* w, void* const* y, void* stream) {

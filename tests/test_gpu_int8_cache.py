@@ -125,6 +125,47 @@ def test_append_off_the_16_byte_boundary():
         assert np.array_equal(x, y)
 
 
+@pytest.mark.parametrize("hq,hkv,d,B", [(8, 2, 64, 16), (28, 4, 128, 32), (5, 5, 128, 64), (32, 1, 64, 64), (4, 4, 128, 16)])
+def test_single_tokens_store_what_an_append_stores(hq, hkv, d, B):
+    """Steps of one token a sequence in a pool with a workspace (the decode kernel
+    appends) and without (an append launch): tables, lengths, counts, free stack, codes
+    and exponents are the same, whatever the rows hold; committed or not, two layers,
+    more sequences than a launch, new blocks and empty sequences among them."""
+    log(f"int8 single tokens {hq}/{hkv}/{d} B={B}")
+    geom = W.AttnGeometry(hq, hkv, d)
+    rng = np.random.default_rng(hq + B)
+    n, ctx = 70, [int(x) for x in np.r_[0, 0, B - 1, B, 2 * B, 31, 32, 33, 63, 64, rng.integers(0, 150, 60)]]
+    seqs = [int(x) for x in rng.permutation(n)]
+    blocks = sum(_blocks(c + 5, B) for c in ctx)
+    pools = [_pool(geom, blocks, n, _blocks(160, B), B, n_layers=2, split_q=n, max_splits=4),
+             _pool(geom, blocks, n, _blocks(160, B), B, n_layers=2)]
+    for layer in (0, 1):
+        x = [_bf16(_rand(rng, sum(ctx), h, d)) for h in (hq, hkv, hkv)]
+        for pool in pools:
+            assert pool.replay(layer, seqs, ctx, *x, torch.empty_like(x[0]), 0.09, commit=layer == 1) == 0
+    for step in range(5):
+        for layer in (0, 1):
+            q, k, v = (_rand(rng, n, h, d) for h in (hq, hkv, hkv))
+            k, v = _special_rows(k, 3), _special_rows(v, 6)
+            k[20, hkv - 1, d - 1] = v[21, 0, 9] = np.nan
+            x = [_bf16(t) for t in (q, k, v)]
+            for pool in pools:
+                assert pool.replay(layer, seqs, [1] * n, *x, torch.empty_like(x[0]), 0.09,
+                                   commit=layer == 1 and step != 2) == 0
+        torch.cuda.synchronize()
+        a, b = pools
+        top = int(a.free_top)
+        assert top == int(b.free_top) and torch.equal(a.free_list[:top], b.free_list[:top])
+        assert torch.equal(a.seq_lens, b.seq_lens) and torch.equal(a.ref_counts, b.ref_counts)
+        for s, c in zip(seqs, ctx):
+            m = c + step + (step < 2) + (step == 2)              # step 2 is written over by step 3
+            held = _blocks(m, B)
+            assert torch.equal(a.block_tables[s, :held], b.block_tables[s, :held])
+            for layer in (0, 1):
+                for y, z in zip(_stored(a, layer, s, m), _stored(b, layer, s, m)):
+                    assert np.array_equal(y, z), (step, s, layer)
+
+
 # geometry, block size, kept prefixes, suffixes, contaminated lengths
 PREFILL = [
     (W.AttnGeometry(32, 8, 128), 16, (260, 0, 1000), (301, 77, 129), (600, 50, 1100)),
