@@ -5,9 +5,29 @@
 
 #include <cstdint>
 
+#include "elementwise.h"
 #include "internal.h"
 
 namespace pgsr {
+
+namespace {
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Four outputs of a row: the sums times their scales, plus four bf16 residuals.  Two
+// roundings to fp32 in every kernel (left alone, some tiles' code fuses them into one,
+// and a row's bits would depend on how many rows share its call).
+__device__ __forceinline__ bf16x4 scaled(i32x4 sum, f32x4 scale, bool add, u32x2 r) {
+#pragma clang fp contract(off)
+  f32x4 v = __builtin_convertvector(sum, f32x4) * scale;
+  if (add) v += f32x4{lo_bf16(r[0]), hi_bf16(r[0]), lo_bf16(r[1]), hi_bf16(r[1])};
+  return __builtin_convertvector(v, bf16x4);
+}
+
+}  // namespace
 
 // Up to three products of the same X; their tile columns are numbered through.
 struct Int8Args {

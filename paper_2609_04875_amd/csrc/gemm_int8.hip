@@ -28,7 +28,6 @@
 #include <cmath>
 #include <utility>
 
-#include "elementwise.h"
 #include "gemm_int8.h"
 #include "internal.h"
 
@@ -39,11 +38,6 @@
 namespace pgsr {
 
 namespace {
-
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kSub = 128;              // k per image row (128 bytes)
 constexpr int kCus = 256;
@@ -260,9 +254,7 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) gemm_int8_ring_kernel(Int8A
 #pragma unroll
     for (int i = 0; i < TN; ++i) {
       if (nb + 16 * i >= N) continue;
-      f32x4 v = __builtin_convertvector(acc[i][j], f32x4) * (xsc[j] * wsc[i]);
-      if (p.r) v += f32x4{lo_bf16(rb[i][0]), hi_bf16(rb[i][0]), lo_bf16(rb[i][1]), hi_bf16(rb[i][1])};
-      *(bf16x4*)(p.y + row + nb + 16 * i) = __builtin_convertvector(v, bf16x4);
+      *(bf16x4*)(p.y + row + nb + 16 * i) = scaled(acc[i][j], xsc[j] * wsc[i], p.r != nullptr, rb[i]);
     }
   }
 }

@@ -19,7 +19,6 @@
 
 #include <utility>
 
-#include "elementwise.h"
 #include "gemm_int8.h"
 #include "internal.h"
 
@@ -30,11 +29,6 @@
 namespace pgsr {
 
 namespace {
-
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kGB = 256;               // output tile edge (M and N)
 constexpr int kGK = 128;               // K step (bytes of an image row)
@@ -198,9 +192,7 @@ gemm_int8_wide_kernel(Int8Args a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (nb + 16 * i >= N) continue;
-      f32x4 v = __builtin_convertvector(acc[i][j], f32x4) * (xsc[j] * wsc[i]);
-      if (p.r) v += f32x4{lo_bf16(rb[i][0]), hi_bf16(rb[i][0]), lo_bf16(rb[i][1]), hi_bf16(rb[i][1])};
-      *(bf16x4*)(p.y + row + nb + 16 * i) = __builtin_convertvector(v, bf16x4);
+      *(bf16x4*)(p.y + row + nb + 16 * i) = scaled(acc[i][j], xsc[j] * wsc[i], p.r != nullptr, rb[i]);
     }
   }
 }

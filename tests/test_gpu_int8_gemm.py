@@ -198,6 +198,17 @@ def test_product_bit_exact(m, n, k):
     assert ((out.double() - want).abs() <= bound).all()
 
 
+@pytest.mark.parametrize("m,n,k", PRODUCTS)
+def test_residual_bit_exact(m, n, k):
+    """The product with the scales, then the addition, each rounded to fp32, whatever
+    kernel the size takes: a row's bits depend on its own operands alone."""
+    log(f"gemm_int8 with residual {m} x {n} x {k}")
+    xq, xs, wq, ws = _operands(m, n, k, m + n + k)
+    y = _sum(xq, wq).float() * (xs[:, None] * ws)
+    r = (y * torch.rand(m, n, device="cuda")).to(BF)             # of the product's own size
+    assert torch.equal(gemm_int8(xq, xs, wq, ws, r=r), (y + r.float()).to(BF))
+
+
 def test_extreme_codes():
     """-128 in both operands, sums at the end of int32."""
     for k, code in ((131056, -128), (133136, 127)):
