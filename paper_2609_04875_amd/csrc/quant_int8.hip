@@ -13,7 +13,7 @@
 // One workgroup a row, the whole row in registers: a row is read once and its codes
 // written once, which bounds it (HBM for many rows, one pass through memory and two
 // reductions for a few).  256 threads; 1024 where the rows leave CUs idle, so that one
-// row is in flight at once.
+// row is in flight at once; behind the norm by k alone (launch_front).
 #include <hip/hip_runtime.h>
 
 #include "elementwise.h"
@@ -98,10 +98,11 @@ __device__ inline u32x2 codes8(const float (&y)[8], float s, float r) {
   u32x2 out = {0, 0};
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    float q = y[j] * r;
-    if constexpr (EXACT) q = fmaf(fmaf(-q, s, y[j]), r, q);
-    // |q| <= 127 and a rounding: rint(q) is in the low byte of q + 3 * 2^22
-    const uint32_t b = __float_as_uint(q + 12582912.f);
+    // |q| <= 127 and a rounding: rint(q) is in the low byte of q + 3 * 2^22 (behind the
+    // norm and the gate one operation gives both, in every instantiation)
+    constexpr float kLow = 12582912.f;
+    const float q = y[j] * r;
+    const uint32_t b = __float_as_uint(EXACT ? fmaf(fmaf(-q, s, y[j]), r, q) + kLow : fmaf(y[j], r, kLow));
     out[j / 4] |= (b & 0xFFu) << (8 * (j % 4));
   }
   return out;
@@ -213,7 +214,11 @@ template <int F>
 hipError_t launch_front(int32_t m, int32_t k, const void* x, const void* gain, float eps, void* q, float* scales,
                         hipStream_t st) {
   if (m <= 0) return hipSuccess;
-  if (k > 256 * 8 && (m <= 256 || k > 256 * 8 * 8)) launch_nt<F, 1024>(m, k, x, gain, eps, q, scales, st);
+  // Behind the norm the sum of squares has the threads' order, so their number goes by
+  // k alone: a row's bits do not depend on how many rows share its call.
+  const bool many = F == kNorm ? k > 512 * 8 : k > 256 * 8 && (m <= 256 || k > 256 * 8 * 8);
+  if (many) launch_nt<F, 1024>(m, k, x, gain, eps, q, scales, st);
+  else if (F == kNorm && k > 256 * 8) launch_nt<F, 512>(m, k, x, gain, eps, q, scales, st);
   else launch_nt<F, 256>(m, k, x, gain, eps, q, scales, st);
   return hipGetLastError();
 }

@@ -198,6 +198,20 @@ def test_product_bit_exact(m, n, k):
     assert ((out.double() - want).abs() <= bound).all()
 
 
+@pytest.mark.parametrize("k", [16, 512, 2048, 2064, 4096, 8192, 8208, 18944])
+def test_quantised_rows_do_not_depend_on_the_others(k):
+    """A row's codes and scale in calls of 1, 256, 257 and 2000 rows, bit for bit."""
+    log(f"rows of {k} in calls of different sizes")
+    x = (torch.randn(2000, 2 * k, device="cuda") * 3).to(BF)
+    gain = (torch.randn(k, device="cuda") * 0.3 + 1).to(BF)
+    for f, y in ((lambda t: rmsnorm_int8(t, gain, 1e-5), x[:, :k].contiguous()), (silu_mul_int8, x),
+                 (quantize_rows, x[:, k:].contiguous()), (quantize_rows, x[:, k:].float().contiguous())):
+        q, s = f(y)
+        for m in (1, 256, 257):
+            q2, s2 = f(y[300:300 + m])
+            assert torch.equal(q2, q[300:300 + m]) and torch.equal(s2, s[300:300 + m]), m
+
+
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
 def test_residual_bit_exact(m, n, k):
     """The product with the scales, then the addition, each rounded to fp32, whatever
