@@ -12,8 +12,8 @@
 //
 // One workgroup a row, the whole row in registers: a row is read once and its codes
 // written once, which bounds it (HBM for many rows, one pass through memory and two
-// reductions for a few).  256 threads; 1024 where the rows leave CUs idle, so that one
-// row is in flight at once; behind the norm by k alone (launch_front).
+// reductions for a few).  256 threads; 1024 (behind the norm 512 up to 4096 values) where
+// the rows leave CUs idle, so that one row is in flight at once.
 #include <hip/hip_runtime.h>
 
 #include "elementwise.h"
@@ -118,56 +118,61 @@ __device__ inline u32x2 codes8_far(const float (&y)[8], float s) {
   return out;
 }
 
-// NC chunks of 8 a thread hold the row; NC = 0: a longer row, read twice.
-template <int F, int NT, int NC>
+// NC chunks of 8 a thread hold the row; NC = 0: a longer row, read twice.  The sum of
+// squares has the order of NT * VP threads: a thread keeps the sums of VP of them.
+template <int F, int NT, int NC, int VP>
 __global__ void __launch_bounds__(NT) quantize_kernel(int32_t k, const void* __restrict__ x,
                                                       const uint16_t* __restrict__ gain, float eps,
                                                       uint8_t* __restrict__ q, float* __restrict__ scales) {
   __shared__ uint32_t red_m[NT / 64];
-  __shared__ float red_s[NT / 64];
+  __shared__ float red_s[NT / 64 * VP];
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, chunks = k / 8;
   float y[NC > 0 ? NC : 1][8];
-  float ss = 0.f;
+  float ss[VP] = {};
   uint32_t m = 0;
   if constexpr (NC > 0) {
 #pragma unroll
     for (int i = 0; i < NC; ++i)
-      if (tid + i * NT < chunks) load8<F>(x, gain, row, k, (tid + i * NT) * 8, y[i], ss);
+      if (tid + i * NT < chunks) load8<F>(x, gain, row, k, (tid + i * NT) * 8, y[i], ss[i % VP]);
 #pragma unroll
     for (int i = 0; i < NC; ++i)
       if (tid + i * NT < chunks) m = mag8(y[i], m);
   } else {
     for (int c = tid; c < chunks; c += NT) {
-      load8<F>(x, gain, row, k, c * 8, y[0], ss);
+      load8<F>(x, gain, row, k, c * 8, y[0], ss[0]);
       m = mag8(y[0], m);
     }
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) {
     m = max(m, (uint32_t)__shfl_xor((int)m, off));
-    if constexpr (F == kNorm) ss += __shfl_xor(ss, off);
+    if constexpr (F == kNorm)
+#pragma unroll
+      for (int p = 0; p < VP; ++p) ss[p] += __shfl_xor(ss[p], off);
   }
   if ((tid & 63) == 0) {
     red_m[tid >> 6] = m;
-    if constexpr (F == kNorm) red_s[tid >> 6] = ss;
+    if constexpr (F == kNorm)
+#pragma unroll
+      for (int p = 0; p < VP; ++p) red_s[p * (NT / 64) + (tid >> 6)] = ss[p];
   }
   __syncthreads();
   m = 0;
-  ss = 0.f;
 #pragma unroll
-  for (int w = 0; w < NT / 64; ++w) {
-    m = max(m, red_m[w]);
-    if constexpr (F == kNorm) ss += red_s[w];
-  }
+  for (int w = 0; w < NT / 64; ++w) m = max(m, red_m[w]);
+  float sum = 0.f;
+  if constexpr (F == kNorm)
+#pragma unroll
+    for (int w = 0; w < NT / 64 * VP; ++w) sum += red_s[w];
   float f = 1.f, top = __uint_as_float(m);
   if constexpr (F == kNorm) {
-    f = 1.f / sqrtf(ss / (float)k + eps);
+    f = 1.f / sqrtf(sum / (float)k + eps);
     top *= f;
   }
   // a NaN or an infinity in the row; behind the norm also a row whose mean square is
   // 0 with eps 0 or leaves fp32
-  const bool bad = !(top < INFINITY) || (F == kNorm && !(ss < INFINITY && f < INFINITY));
+  const bool bad = !(top < INFINITY) || (F == kNorm && !(sum < INFINITY && f < INFINITY));
   const float s = bad ? __uint_as_float(0x7FC00000u) : top / 127.f;
   if (tid == 0) scales[row] = s;
   // behind the norm y is x * gain: the row's factor goes into the quotient's divisor
@@ -185,25 +190,25 @@ __global__ void __launch_bounds__(NT) quantize_kernel(int32_t k, const void* __r
       if (tid + i * NT < chunks) *(u32x2*)(out + (tid + i * NT) * 8) = codes(y[i]);
   } else {
     for (int c = tid; c < chunks; c += NT) {
-      load8<F>(x, gain, row, k, c * 8, y[0], ss);
+      load8<F>(x, gain, row, k, c * 8, y[0], ss[0]);
       *(u32x2*)(out + c * 8) = codes(y[0]);
     }
   }
 }
 
-template <int F, int NT>
+template <int F, int NT, int VP = 1>
 void launch_nt(int32_t m, int32_t k, const void* x, const void* gain, float eps, void* q, float* scales, hipStream_t st) {
   const int per = (k / 8 + NT - 1) / NT;
   auto go = [&](auto nc) {
     constexpr int32_t kRows = 1 << 21;             // a launch counts its threads in 32 bits
     for (int32_t r0 = 0; r0 < m; r0 += kRows) {
       const int64_t at = (int64_t)r0 * k * (F == kRowsF32 || F == kGate ? 4 : 2);
-      hipLaunchKernelGGL((quantize_kernel<F, NT, decltype(nc)::value>), dim3(min(kRows, m - r0)), dim3(NT), 0, st, k,
+      hipLaunchKernelGGL((quantize_kernel<F, NT, decltype(nc)::value, VP>), dim3(min(kRows, m - r0)), dim3(NT), 0, st, k,
                          (const char*)x + at, (const uint16_t*)gain, eps, (uint8_t*)q + (int64_t)r0 * k, scales + r0);
       if (m - r0 <= kRows) break;
     }
   };
-  if (per <= 1) go(std::integral_constant<int, 1>{});
+  if (per <= VP) go(std::integral_constant<int, VP>{});   // VP > 1: rows of more than NT chunks
   else if (per <= 2) go(std::integral_constant<int, 2>{});
   else if (per <= 4) go(std::integral_constant<int, 4>{});
   else if (per <= 8 && NT == 256) go(std::integral_constant<int, NT == 256 ? 8 : 0>{});
@@ -214,12 +219,20 @@ template <int F>
 hipError_t launch_front(int32_t m, int32_t k, const void* x, const void* gain, float eps, void* q, float* scales,
                         hipStream_t st) {
   if (m <= 0) return hipSuccess;
-  // Behind the norm the sum of squares has the threads' order, so their number goes by
-  // k alone: a row's bits do not depend on how many rows share its call.
-  const bool many = F == kNorm ? k > 512 * 8 : k > 256 * 8 && (m <= 256 || k > 256 * 8 * 8);
-  if (many) launch_nt<F, 1024>(m, k, x, gain, eps, q, scales, st);
-  else if (F == kNorm && k > 256 * 8) launch_nt<F, 512>(m, k, x, gain, eps, q, scales, st);
-  else launch_nt<F, 256>(m, k, x, gain, eps, q, scales, st);
+  if constexpr (F == kNorm) {
+    // The order of the sum of squares goes by k alone, so that a row's bits do not depend
+    // on how many rows share its call: 256, 512 or 1024 threads' (2048 rows of 4096 in
+    // 512 threads 13.6 us, in 256 with the sums of two each 9.3).
+    if (k <= 256 * 8) launch_nt<F, 256>(m, k, x, gain, eps, q, scales, st);
+    else if (k <= 512 * 8 && m <= 256) launch_nt<F, 512>(m, k, x, gain, eps, q, scales, st);
+    else if (k <= 512 * 8) launch_nt<F, 256, 2>(m, k, x, gain, eps, q, scales, st);
+    else if (m <= 256 || k > 256 * 8 * 8) launch_nt<F, 1024>(m, k, x, gain, eps, q, scales, st);
+    else launch_nt<F, 256, 4>(m, k, x, gain, eps, q, scales, st);
+  } else if (k > 256 * 8 && (m <= 256 || k > 256 * 8 * 8)) {
+    launch_nt<F, 1024>(m, k, x, gain, eps, q, scales, st);
+  } else {
+    launch_nt<F, 256>(m, k, x, gain, eps, q, scales, st);
+  }
   return hipGetLastError();
 }
 
