@@ -1,9 +1,11 @@
-// What the int8 product's kernels share (gemm_int8.hip, gemm_int8_wide.hip).
+// What the int8 product's kernels share (gemm_int8.hip, gemm_int8_ring.hip,
+// gemm_int8_wide.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <utility>
 
 #include "elementwise.h"
 #include "internal.h"
@@ -16,6 +18,22 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kSub = 128;              // k of an image row (bytes)
+
+template <class F, int... I>
+__device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+// swizzle of the 16-byte chunk slot within a 128-byte image row
+__device__ __forceinline__ int gsw(int row) { return (row >> 1) & 7; }
+
+// all but this wave's latest N requests, and its LDS reads, complete
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
 
 // Four outputs of a row: the sums times their scales, plus four bf16 residuals.  Two
 // roundings to fp32 in every kernel (left alone, some tiles' code fuses them into one,
@@ -63,7 +81,9 @@ __device__ __forceinline__ Int8Side int8_side(const Int8Args& a, int& tn) {
   return p;
 }
 
-// One wave per SIMD and 256 x 256 tiles: K a multiple of 128.
-hipError_t launch_gemm_int8_wide(const Int8Args& a, hipStream_t s);
+// Tiles of 128 x 64, 128 x 128 and 256 x 128 (bm x bn), eight waves.
+hipError_t launch_gemm_int8_ring(const Int8Args& a, int bm, int bn, hipStream_t s);
+// One wave per SIMD and tiles of 256 x bn, bn 128 or 256: K a multiple of 128.
+hipError_t launch_gemm_int8_wide(const Int8Args& a, int bn, hipStream_t s);
 
 }  // namespace pgsr

@@ -8,16 +8,18 @@
 // conversion to fp32 rounds sums past 2^24 by half a step of fp32.  Integer sums have no
 // order, so a result depends on no tile, and rows not on which rows share the launch.
 //
-// Tiles from 16 x 16 (one wave: a re-decoded token against a model's weights) to
-// 256 x 128 (eight waves), X and W brought to LDS by global->LDS loads through a ring
-// of NST stages, in the scheme of the bf16 kernels (gemm_bf16_dma.hip): a stage is KSUB
-// images of 128 k (128-byte rows of X, then of W), a request 8 rows x 128 bytes with
-// chunk c of row j in slot c ^ ((j / 2) mod 8); a wave waits for its own requests of the
-// next stage (vmcnt, exact), meets the others at one barrier, reads the next operand
-// group and refills the slot that the barrier freed, ahead of the products of the
-// operands in registers.  An instruction takes the same bytes of both operands and the
-// same cycles as the bf16 one and does twice the work, so a stage of 128 k costs what
-// one of 64 k costs there.
+// This file: the choice of the tile, and the kernel of tiles from 16 x 16 to 64 x 64.
+// Its four waves share the tile's outputs and split K: wave w takes the 128-k stages
+// w, w + 4, ... through a ring of its own in LDS (global->LDS loads: a request is 8 rows
+// x 128 bytes, chunk c of row j in slot c ^ ((j / 2) mod 8)), waits for its own requests
+// alone, and meets the others at the end, where they add up their sums.  No barrier in
+// the loop, each byte read from LDS once, and four stages of K at a time from a handful
+// of rows: against four waves that split the outputs, 1 x 3584 x 18944 17.2 -> 12.4 us,
+// 1 x 28672 x 4096 22.8 -> 19.5, 102 x 4096 x 14336 24.4 -> 23.7, 200 rows 30.3 -> 28.5.
+// Few rows stream W from HBM once.  From 64 rows on what bounds it is the lines that a
+// CU can have on their way: some 110 of 128 bytes, each 490 cycles on average where a
+// quarter come from HBM (102 x 3584 x 18944: 76 GB/s a CU, 125 with every line in L2),
+// so larger tiles pay as soon as they fill the CUs, and LDS or the products do not.
 //
 // K any multiple of 16: the last stage clamps the chunks past K to the row's last
 // one, and their operands of X are cleared in registers (W's may hold anything:
@@ -39,41 +41,23 @@ namespace pgsr {
 
 namespace {
 
-constexpr int kSub = 128;              // k per image row (128 bytes)
 constexpr int kCus = 256;
-
-template <class F, int... I>
-__device__ __forceinline__ void static_for(F&& f, std::integer_sequence<int, I...>) {
-  (f(std::integral_constant<int, I>{}), ...);
-}
-
-// swizzle of the 16-byte chunk slot within a 128-byte image row
-__device__ __forceinline__ int gsw(int row) { return (row >> 1) & 7; }
-
-// all but this wave's latest N requests, and its LDS reads, complete
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
-}
+constexpr int kWaves = 4;
+constexpr int kGroupM = 8;             // tile rows per group of the tile order
 
 // ONCE: one tile row, so no other tile reads this W: non-temporal requests.
-template <int BM, int BN, int WGM, int WGN, int KSUB, int NST, int GS, int GM, bool ONCE>
-__global__ void __launch_bounds__(WGM * WGN * 64, 1) gemm_int8_ring_kernel(Int8Args a) {
-  constexpr int NW = WGM * WGN;
-  constexpr int TM = BM / WGM / 16, TN = BN / WGN / 16;
-  constexpr int XR = BM / 8 / NW, WR = BN / 8 / NW;       // 1 KB runs per wave and sub-image
-  static_assert(XR * NW * 8 == BM && WR * NW * 8 == BN, "runs split evenly over the waves");
-  constexpr int RPW = KSUB * (XR + WR);                    // requests per wave and stage
-  static_assert(RPW * (NST - 1) <= 63, "vmcnt range");
-  constexpr int SUBE = (BM + BN) * kSub, STE = KSUB * SUBE;   // bytes of a sub-image pair, a stage
-  constexpr int KST = kSub * KSUB;                         // k of a stage
-  constexpr int NKS = 2 * KSUB;                            // k slices of 64 per stage
-  constexpr int NG = NKS / GS;                             // operand groups of GS slices per stage
-  static_assert(NKS % GS == 0 && (NG == 1 || NG % 2 == 0), "operand groups");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[NST * STE];
+template <int BM, int BN, int NST, bool ONCE>
+__global__ void __launch_bounds__(kWaves * 64, 1) gemm_int8_kernel(Int8Args a) {
+  constexpr int TM = BM / 16, TN = BN / 16;
+  constexpr int XR = BM / 8, WR = BN / 8;                  // requests of 8 rows x 128 bytes
+  constexpr int RPS = XR + WR;                             // a wave's, of one stage
+  static_assert(RPS * (NST - 1) <= 63, "vmcnt range");
+  constexpr int STE = (BM + BN) * kSub;                    // bytes of a stage: rows of X, then of W
+  constexpr int RING = kWaves * NST * STE, SUMS = TM * TN * kWaves * 1024;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[RING > SUMS ? RING : SUMS];
 
   // output tile of this workgroup: XCD x = blockIdx % 8 takes tiles
-  // [x * per_xcd, (x + 1) * per_xcd), in groups of GM tile rows (the tile rows
+  // [x * per_xcd, (x + 1) * per_xcd), in groups of kGroupM tile rows (the tile rows
   // of one W panel run side by side on one XCD, so its L2 takes W once)
   const int M = a.m, K = a.k;
   const int n_tm = (M + BM - 1) / BM;
@@ -83,106 +67,58 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) gemm_int8_ring_kernel(Int8A
   const int per_xcd = (n_tm * n_tn + 7) / 8;
   const int t = (int)(blockIdx.x % 8) * per_xcd + (int)(blockIdx.x / 8);
   if (t >= n_tm * n_tn) return;
-  const int grp = t / (GM * n_tn), first_m = grp * GM;
-  const int gsize = min(n_tm - first_m, GM);
-  const int idx = t - grp * GM * n_tn;
+  const int grp = t / (kGroupM * n_tn), first_m = grp * kGroupM;
+  const int gsize = min(n_tm - first_m, kGroupM);
+  const int idx = t - grp * kGroupM * n_tn;
   const int m0 = (first_m + idx % gsize) * BM;
   int tn = idx / gsize;
   const Int8Side p = int8_side<BN>(a, tn);
   const int N = p.n;
   const int n0 = tn * BN;
 
-  const int tid = threadIdx.x;
-  const int w = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lane = tid & 63, r16 = lane & 15, g4 = lane >> 4;
-  const int wm = (w % WGM) * TM * 16, wn = (w / WGM) * TN * 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, r16 = lane & 15, g4 = lane >> 4;
 
-  // This lane's requests: run j holds rows 8 (w + NW j) + lane / 8; rows past M or
-  // N read row M-1 or N-1 (never stored).  Offsets from the tile's first row.
+  // This lane's requests: run j holds rows 8 j + lane / 8; rows past M or N read row
+  // M-1 or N-1 (never stored).  Offsets from the tile's first row.
   const char* const X0 = (const char*)a.x + (int64_t)m0 * K;
   const char* const W0 = (const char*)p.w + (int64_t)n0 * K;
   uint32_t xrow[XR], wrow[WR];
-  int xc[XR], wc[WR];                              // chunk of the image row this lane fetches
 #pragma unroll
-  for (int j = 0; j < XR; ++j) {
-    const int row = 8 * (w + NW * j) + lane / 8;
-    xrow[j] = (uint32_t)(min(m0 + row, M - 1) - m0) * (uint32_t)K;
-    xc[j] = (lane & 7) ^ gsw(row);
-  }
+  for (int j = 0; j < XR; ++j) xrow[j] = (uint32_t)(min(m0 + 8 * j + lane / 8, M - 1) - m0) * (uint32_t)K;
 #pragma unroll
-  for (int j = 0; j < WR; ++j) {
-    const int row = 8 * (w + NW * j) + lane / 8;
-    wrow[j] = (uint32_t)(min(n0 + row, N - 1) - n0) * (uint32_t)K;
-    wc[j] = (lane & 7) ^ gsw(row);
-  }
-  const uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0] + 1024u * w;
-  const int nst = (K + KST - 1) / KST;
-  const int last_chunks = (K - (nst - 1) * KST) / 16;      // of the last stage, 1 .. 8 KSUB
-  auto request = [&](int st, int slot) {
-    const char* xs = X0 + (int64_t)st * KST;
-    const char* ws = W0 + (int64_t)st * KST;
+  for (int j = 0; j < WR; ++j) wrow[j] = (uint32_t)(min(n0 + 8 * j + lane / 8, N - 1) - n0) * (uint32_t)K;
+  // chunk of the image row this lane fetches, even and odd runs
+  const int chunk[2] = {(lane & 7) ^ gsw(lane / 8), (lane & 7) ^ gsw(8 + lane / 8)};
+  const uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0] + (uint32_t)(w * NST * STE);
+  const int nst = (K + kSub - 1) / kSub;
+  const int last_chunks = (K - (nst - 1) * kSub) / 16;     // of the last stage, 1 .. 8
+  const int mine = (nst - w + kWaves - 1) / kWaves;        // this wave's stages: w, w + kWaves, ..
+  auto request = [&](int i, int slot) {
+    const int st = w + kWaves * i;
+    const char* xs = X0 + (int64_t)st * kSub;
+    const char* ws = W0 + (int64_t)st * kSub;
     const uint32_t img = lds0 + (uint32_t)(slot * STE);
-    const int most = (st == nst - 1 ? last_chunks : 8 * KSUB) - 1;
+    const int most = (st == nst - 1 ? last_chunks : 8) - 1;
+    const uint32_t c[2] = {16u * (uint32_t)min(chunk[0], most), 16u * (uint32_t)min(chunk[1], most)};
 #pragma unroll
-    for (int sub = 0; sub < KSUB; ++sub) {
-#pragma unroll
-      for (int j = 0; j < WR; ++j) {
-        const uint32_t off = wrow[j] + 16u * (uint32_t)min(8 * sub + wc[j], most);
-        if constexpr (ONCE)
-          asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
-                       ::"v"(off), "s"(ws), "s"(img + (uint32_t)(sub * SUBE + BM * kSub) + 1024u * NW * j)
-                       : "memory", "m0");
-        else
-          asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                       ::"v"(off), "s"(ws), "s"(img + (uint32_t)(sub * SUBE + BM * kSub) + 1024u * NW * j)
-                       : "memory", "m0");
-      }
-#pragma unroll
-      for (int j = 0; j < XR; ++j) {
-        const uint32_t off = xrow[j] + 16u * (uint32_t)min(8 * sub + xc[j], most);
+    for (int j = 0; j < WR; ++j) {
+      if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+                     ::"v"(wrow[j] + c[j & 1]), "s"(ws), "s"(img + (uint32_t)(BM * kSub + 1024 * j)) : "memory", "m0");
+      else
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
-                     ::"v"(off), "s"(xs), "s"(img + (uint32_t)(sub * SUBE) + 1024u * NW * j)
-                     : "memory", "m0");
-      }
+                     ::"v"(wrow[j] + c[j & 1]), "s"(ws), "s"(img + (uint32_t)(BM * kSub + 1024 * j)) : "memory", "m0");
     }
+#pragma unroll
+    for (int j = 0; j < XR; ++j)
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                   ::"v"(xrow[j] + c[j & 1]), "s"(xs), "s"(img + (uint32_t)(1024 * j)) : "memory", "m0");
   };
   // this wave's requests complete but for those of the latest `ahead` stages
-  // (its LDS reads too), and every other wave's at the barrier
   auto landed = [&](int ahead) {
-    if (ahead >= NST - 2) wait_loads<RPW * (NST - 2)>();
-    else
-      static_for([&](auto ic) { if (ahead == decltype(ic)::value) wait_loads<RPW * decltype(ic)::value>(); },
-                 std::make_integer_sequence<int, (NST > 2 ? NST - 2 : 1)>{});
-    if constexpr (NW > 1) asm volatile("s_barrier" ::: "memory");
-  };
-
-  // operand = 16 rows x 64 k: lane l -> row l % 16, chunk l / 16 of the slice
-  int soff[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) soff[h] = r16 * kSub + (((4 * h + g4) ^ gsw(r16)) << 4);
-  i32x4 wa[2][GS][TN], xb[2][GS][TM];
-  // operand group grp of the stage in `slot`; `last`: its chunks of X past K are cleared
-  auto read_ops = [&](int slot, int grp, bool last, auto set_c) {
-    constexpr int set = decltype(set_c)::value;
-#pragma unroll
-    for (int h = 0; h < GS; ++h) {
-      const int ks = grp * GS + h;
-      const uint8_t* img = &lds[slot * STE + (ks / 2) * SUBE];
-#pragma unroll
-      for (int i = 0; i < TN; ++i) wa[set][h][i] = *(const i32x4*)&img[(BM + wn + 16 * i) * kSub + soff[ks & 1]];
-#pragma unroll
-      for (int j = 0; j < TM; ++j) xb[set][h][j] = *(const i32x4*)&img[(wm + 16 * j) * kSub + soff[ks & 1]];
-    }
-    if (last) {
-#pragma unroll
-      for (int h = 0; h < GS; ++h) {
-        const bool in = 4 * (grp * GS + h) + g4 < last_chunks;
-#pragma unroll
-        for (int j = 0; j < TM; ++j)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) xb[set][h][j][q] = in ? xb[set][h][j][q] : 0;
-      }
-    }
+    static_for([&](auto ic) { if (ahead == decltype(ic)::value) wait_loads<RPS * decltype(ic)::value>(); },
+               std::make_integer_sequence<int, NST>{});
   };
 
   i32x4 acc[TN][TM];
@@ -191,112 +127,121 @@ __global__ void __launch_bounds__(WGM * WGN * 64, 1) gemm_int8_ring_kernel(Int8A
 #pragma unroll
     for (int j = 0; j < TM; ++j) acc[i][j] = i32x4{};
 
-  const bool ragged = last_chunks != 8 * KSUB;
 #pragma unroll
-  for (int st = 0; st < NST - 1; ++st)
-    if (st < nst) request(st, st);
-  landed(min(NST - 1, nst) - 1);
-  if (NST - 1 < nst) request(NST - 1, NST - 1);
-  read_ops(0, 0, ragged && nst == 1, std::integral_constant<int, 0>{});
-
+  for (int i = 0; i < NST; ++i)
+    if (i < mine) request(i, i);
   int slot = 0;
-  // stage s from ring slot `slot`, its first operand group in set par
-  auto stage = [&](int s, auto par_c) {
-    constexpr int par = decltype(par_c)::value;
-    const int nslot = slot + 1 == NST ? 0 : slot + 1;
-    static_for([&](auto gc) {
-      constexpr int g = decltype(gc)::value, cur = (par + g) & 1;
-      if constexpr (g < NG - 1) {
-        read_ops(slot, g + 1, ragged && s == nst - 1, std::integral_constant<int, 1 - cur>{});
-      } else if (s + 1 < nst) {
-        landed(min(NST - 2, nst - 2 - s));
-        read_ops(nslot, 0, ragged && s == nst - 2, std::integral_constant<int, 1 - cur>{});
-        if (s + NST < nst) request(s + NST, slot);
-      }
+  for (int i = 0; i < mine; ++i) {
+    landed(min(NST - 1, mine - 1 - i));
+    // operand = 16 rows x 64 k: lane l -> row l % 16, chunk l / 16 of the slice
+    const uint8_t* img = &lds[(w * NST + slot) * STE];
+    i32x4 wa[2][TN], xb[2][TM];
 #pragma unroll
-      for (int h = 0; h < GS; ++h)
+    for (int h = 0; h < 2; ++h) {
+      const int off = r16 * kSub + (((4 * h + g4) ^ gsw(r16)) << 4);
 #pragma unroll
-        for (int i = 0; i < TN; ++i)
+      for (int q = 0; q < TN; ++q) wa[h][q] = *(const i32x4*)&img[(BM + 16 * q) * kSub + off];
 #pragma unroll
-          for (int j = 0; j < TM; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wa[cur][h][i], xb[cur][h][j], acc[i][j], 0, 0, 0);
-    }, std::make_integer_sequence<int, NG>{});
-    slot = nslot;
-  };
-  int s = 0;
-  for (; s + 1 < nst; s += 2) {
-    stage(s, std::integral_constant<int, 0>{});
-    stage(s + 1, std::integral_constant<int, NG & 1>{});
+      for (int q = 0; q < TM; ++q) xb[h][q] = *(const i32x4*)&img[16 * q * kSub + off];
+    }
+    if (last_chunks != 8 && w + kWaves * i == nst - 1) {   // chunks of X past K are cleared
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int q = 0; q < TM; ++q)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) xb[h][q][c] = 4 * h + g4 < last_chunks ? xb[h][q][c] : 0;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the slot is read: it takes stage i + NST
+    if (i + NST < mine) request(i + NST, slot);
+    slot = slot + 1 == NST ? 0 : slot + 1;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int q = 0; q < TN; ++q)
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+          acc[q][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wa[h][q], xb[h][j], acc[q][j], 0, 0, 0);
   }
-  if (s < nst) stage(s, std::integral_constant<int, 0>{});
 
-  // acc[i][j] lane l, register q: n = wn + 16 i + 4 (l / 16) + q, m = wm + 16 j + l % 16.
-  // Scales, and a row's residuals, are asked for ahead of the stores that could (as far
-  // as the compiler knows) change them.
-  const int nb = n0 + wn + 4 * g4;                 // N is a multiple of 8: whole groups in or out
-  f32x4 wsc[TN];
+  // The waves' sums: sub-tile u is added up and stored by wave u % kWaves, which takes
+  // the others' from LDS (every ring is read: the barrier).
+  __syncthreads();
 #pragma unroll
-  for (int i = 0; i < TN; ++i) wsc[i] = *(const f32x4*)(p.ws + min(nb + 16 * i, N - 4));
-  float xsc[TM];
+  for (int u = 0; u < TN * TM; ++u)
+    if (w != u % kWaves) *(i32x4*)&lds[(u * kWaves + w) * 1024 + lane * 16] = acc[u / TM][u % TM];
+  // acc[i][j] lane l, register q: n = 16 i + 4 (l / 16) + q, m = 16 j + l % 16.
+  // Scales and residuals are asked for ahead of the stores that could (as far as the
+  // compiler knows) change them.
+  constexpr int OWN = (TN * TM + kWaves - 1) / kWaves;
+  f32x4 wsc[OWN];
+  float xsc[OWN];
+  u32x2 rb[OWN];
+  const int nb = n0 + 4 * g4;                      // N is a multiple of 8: whole groups in or out
 #pragma unroll
-  for (int j = 0; j < TM; ++j) xsc[j] = a.xs[min(m0 + wm + 16 * j + r16, M - 1)];
+  for (int v = 0; v < OWN; ++v) {
+    const int u = v * kWaves + w, n = nb + 16 * (u / TM), m = m0 + 16 * (u % TM) + r16;
+    wsc[v] = *(const f32x4*)(p.ws + min(n, N - 4));
+    xsc[v] = a.xs[min(m, M - 1)];
+    if (p.r && u < TN * TM && m < M && n < N) rb[v] = *(const u32x2*)(p.r + (int64_t)m * N + n);
+  }
+  __syncthreads();
 #pragma unroll
-  for (int j = 0; j < TM; ++j) {
-    const int m = m0 + wm + 16 * j + r16;
-    if (m >= M) continue;
-    const int64_t row = (int64_t)m * N;
-    u32x2 rb[TN];
-    if (p.r) {
+  for (int u = 0; u < TN * TM; ++u) {
+    if (w != u % kWaves) continue;
+    i32x4 sum = acc[u / TM][u % TM];
 #pragma unroll
-      for (int i = 0; i < TN; ++i)
-        if (nb + 16 * i < N) rb[i] = *(const u32x2*)(p.r + row + nb + 16 * i);
-    }
-#pragma unroll
-    for (int i = 0; i < TN; ++i) {
-      if (nb + 16 * i >= N) continue;
-      *(bf16x4*)(p.y + row + nb + 16 * i) = scaled(acc[i][j], xsc[j] * wsc[i], p.r != nullptr, rb[i]);
-    }
+    for (int o = 1; o < kWaves; ++o) sum += *(const i32x4*)&lds[(u * kWaves + (u + o) % kWaves) * 1024 + lane * 16];
+    const int n = nb + 16 * (u / TM), m = m0 + 16 * (u % TM) + r16;
+    if (m >= M || n >= N) continue;
+    *(bf16x4*)(p.y + (int64_t)m * N + n) =
+        scaled(sum, xsc[u / kWaves] * wsc[u / kWaves], p.r != nullptr, rb[u / kWaves]);
   }
 }
 
-template <int BM, int BN, int WGM, int WGN, int KSUB, int NST, int GS, int GM>
-void launch_ring(const Int8Args& a, hipStream_t s) {
+template <int BM, int BN, int NST>
+void launch_tile(const Int8Args& a, hipStream_t s) {
   int64_t cols = 0;
   for (int i = 0; i < a.count; ++i) cols += (a.n[i] + BN - 1) / BN;
   const int64_t tiles = (int64_t)((a.m + BM - 1) / BM) * cols;
-  const dim3 grid((unsigned)(8 * ((tiles + 7) / 8))), blk(WGM * WGN * 64);
-  if (a.m <= BM)
-    hipLaunchKernelGGL((gemm_int8_ring_kernel<BM, BN, WGM, WGN, KSUB, NST, GS, GM, true>), grid, blk, 0, s, a);
-  else
-    hipLaunchKernelGGL((gemm_int8_ring_kernel<BM, BN, WGM, WGN, KSUB, NST, GS, GM, false>), grid, blk, 0, s, a);
+  const dim3 grid((unsigned)(8 * ((tiles + 7) / 8))), blk(kWaves * 64);
+  if (a.m <= BM) hipLaunchKernelGGL((gemm_int8_kernel<BM, BN, NST, true>), grid, blk, 0, s, a);
+  else hipLaunchKernelGGL((gemm_int8_kernel<BM, BN, NST, false>), grid, blk, 0, s, a);
 }
 
 // Tile choice: the time of a launch is close to
 //   max(1, 0.36 r + 0.64 ceil(r)) * (K / 128 * step + fix),   r = tiles / 256 CUs
 // (a partly filled last round costs most of a whole one): one 128-k step of one tile
-// per CU, and a tile's prologue and epilogue.  step and fix are the fit to 148 products
+// per CU, and a tile's prologue and epilogue.  step and fix are fitted to 311 products
 // (M 1 to 4096; N and K of three models' projections and smaller ones, W out of the
-// caches), where the tile it picks is 1.1% slower than the fastest of the nine on
-// average and 13% at most (102 x 4096 x 4096 in 64 x 32 tiles 9.5 us, 32 x 32 8.4).
+// caches), where the tile it picks is 0.6% slower than the fastest of the eleven on
+// average and 12% at most (1 x 8192 x 28672 in 32 x 32 tiles 42.3 us, 16 x 16 37.9).
+// 16 x 16 tiles in number run rings of two stages, five workgroups to a CU (1 x 28672 x
+// 4096 19.5 us, four stages 22.3; 1 x 57344 x 8192 66.1, 68.5), few of them four (1 x
+// 3584 x 18944 12.4 us, two stages 16.5; 1 x 8192 x 28672 37.7, 40.7).
 struct TileCost {
   int bm, bn;
   double step_ns, fix_ns;
 };
-constexpr TileCost kTiles[] = {{16, 16, 64, 837},     {32, 16, 87, 1737},    {32, 32, 107, 1129},
-                               {64, 32, 162, 2156},   {64, 64, 229, 2197},   {128, 64, 348, 1912},
-                               {128, 128, 601, 1587}, {256, 128, 963, 1731}, {256, 256, 1504, 674}};
-constexpr int kWide = 8;               // gemm_int8_wide.hip; K a multiple of 128
+constexpr TileCost kTiles[] = {{16, 16, 57, 888},     {16, 16, 50, 494},     {32, 16, 60, 683},    {32, 32, 103, 858},
+                               {64, 32, 150, 2129},   {64, 64, 265, 2478},   {128, 64, 354, 1809}, {128, 128, 588, 1730},
+                               {256, 128, 920, 2537}, {256, 128, 863, 3144}, {256, 256, 1529, 2340}};
+constexpr int kDeep = 0, kShallow = 1; // 16 x 16 by the number of tiles
+constexpr int kManyTiles = 4 * kCus;
+constexpr int kWide = 9;               // from here on gemm_int8_wide.hip: K a multiple of 128
 
 int pick_tile(int m, int k, int count, const int* n) {
-  int best = 0;
+  int best = -1;
   double best_cost = 0;
-  for (int i = 0; i <= (k % 128 == 0 ? kWide : kWide - 1); ++i) {
+  for (int i = 0; i < (k % 128 == 0 ? kWide + 2 : kWide); ++i) {
     const TileCost& t = kTiles[i];
     double cols = 0;
     for (int j = 0; j < count; ++j) cols += ((int64_t)n[j] + t.bn - 1) / t.bn;
-    const double r = (double)(((int64_t)m + t.bm - 1) / t.bm) * cols / kCus;
+    const double tiles = (double)(((int64_t)m + t.bm - 1) / t.bm) * cols, r = tiles / kCus;
+    if (i == (tiles > kManyTiles ? kDeep : kShallow)) continue;
+    if (tiles * 512 >= 4294967296.0) continue;     // a launch counts its threads in 32 bits
     const double cost = (r <= 1.0 ? 1.0 : 0.36 * r + 0.64 * ceil(r)) * ((k + 127) / 128 * t.step_ns + t.fix_ns);
-    if (i == 0 || cost < best_cost) {
+    if (best < 0 || cost < best_cost) {
       best = i;
       best_cost = cost;
     }
@@ -306,28 +251,28 @@ int pick_tile(int m, int k, int count, const int* n) {
 
 hipError_t run_tile(int tile, const Int8Args& a, hipStream_t s) {
   switch (tile) {
-    case 0: launch_ring<16, 16, 1, 1, 2, 8, 4, 8>(a, s); break;
-    case 1: launch_ring<32, 16, 2, 1, 2, 8, 4, 8>(a, s); break;
-    case 2: launch_ring<32, 32, 2, 2, 2, 4, 4, 8>(a, s); break;
-    case 3: launch_ring<64, 32, 2, 2, 2, 6, 2, 8>(a, s); break;
-    case 4: launch_ring<64, 64, 2, 2, 2, 4, 2, 8>(a, s); break;
-    case 5: launch_ring<128, 64, 4, 2, 2, 3, 2, 8>(a, s); break;
-    case 6: launch_ring<128, 128, 4, 2, 1, 4, 1, 8>(a, s); break;
-    case 7: launch_ring<256, 128, 4, 2, 1, 3, 1, 4>(a, s); break;
-    default: return launch_gemm_int8_wide(a, s);
+    case kDeep: launch_tile<16, 16, 4>(a, s); break;
+    case kShallow: launch_tile<16, 16, 2>(a, s); break;
+    case 2: launch_tile<32, 16, 3>(a, s); break;
+    case 3: launch_tile<32, 32, 2>(a, s); break;
+    case 4: launch_tile<64, 32, 3>(a, s); break;
+    case 5: launch_tile<64, 64, 2>(a, s); break;
+    case 6:
+    case 7:
+    case 8: return launch_gemm_int8_ring(a, kTiles[tile].bm, kTiles[tile].bn, s);
+    default: return launch_gemm_int8_wide(a, kTiles[tile].bn, s);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-// A launch counts its threads in 32 bits: at most 512 to a tile of 256 x 128, 64 to
-// one of 16 x 16, so for any choice no more than 64 for 16 x 16 outputs, with edges of
-// whole 256 x 128 tiles.
+// m * n below 2^34 in whole tiles of 256 x 128, which leaves 2^19 of those: one tile at
+// least that any such size can take in one launch.
 bool gemm_int8_fits(int m, int count, const int* n) {
   double cols = 0;
-  for (int i = 0; i < count; ++i) cols += ((int64_t)n[i] + 127) / 128 * 8;
-  return (double)(((int64_t)m + 255) / 256 * 16) * cols * 64 < 4294967296.0;
+  for (int i = 0; i < count; ++i) cols += ((int64_t)n[i] + 127) / 128;
+  return (double)(((int64_t)m + 255) / 256) * cols < 524288.0;
 }
 
 hipError_t launch_gemm_int8(int m, int k, int count, const int* n, const void* x, const float* xs,

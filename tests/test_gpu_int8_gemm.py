@@ -179,7 +179,9 @@ def _want(xq, xs, wq, ws):
 PRODUCTS = [(1, 8, 16), (1, 4096, 4096), (2, 1024, 144), (3, 16, 32), (16, 24, 48), (17, 40, 112), (31, 1000, 128),
             (33, 264, 240), (64, 512, 256), (65, 2056, 272), (102, 3584, 18944), (128, 128, 384), (129, 136, 1232),
             (300, 4104, 4112), (333, 1000, 1232), (1000, 1000, 1008), (1025, 2048, 2064), (2048, 4096, 512),
-            (2049, 4104, 528), (4096, 8192, 1024), (4100, 8200, 656), (70000, 8, 16), (5, 128256, 64), (1, 8, 133136)]
+            (2049, 4104, 528), (4096, 8192, 1024), (4100, 8200, 656), (70000, 8, 16), (5, 128256, 64), (1, 8, 133136),
+            (9, 20008, 4112), (40, 200, 8208), (201, 3592, 1168), (700, 8200, 1152), (2049, 2056, 2176), (16, 16392, 1024),
+            (7, 3592, 18960)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
