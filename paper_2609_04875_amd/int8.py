@@ -20,55 +20,54 @@ _DT = {torch.float32: N.F32, torch.bfloat16: N.BF16}
 Rows = Tuple[torch.Tensor, torch.Tensor]
 
 
-def _device(x: torch.Tensor, name: str) -> int:
-    """Index of the device ``x`` is on, which must be the current one: kernels are
-    launched there."""
+def _matrix(x: torch.Tensor, name: str):
+    """Rows, columns and device of a matrix, which must be on the current device:
+    kernels are launched there.  A re-decode step is as long as its calls take on the
+    host, so these checks and those of ``_at`` are few and plain."""
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} is {tuple(shape)}; it must be a matrix")
     dv = x.get_device()
     if dv < 0 or dv != torch.cuda.current_device():
         raise ValueError(f"{name} is on {x.device}; the current device is cuda:{torch.cuda.current_device()}")
-    return dv
+    m, k = shape
+    return m, k, dv
 
 
 def _at(t: torch.Tensor, dtype: torch.dtype, name: str, dv: int, numel: int) -> Optional[int]:
-    """``_dev_ptr`` with the checks that pass first: a re-decode step is as long as
-    its calls take on the host."""
+    """``_dev_ptr`` with the checks that pass first."""
     if t.dtype is dtype and t.get_device() == dv and t.is_contiguous() and t.numel() == numel and numel:
         return t.data_ptr()
     return _dev_ptr(t, dtype, name, dv, numel)
 
 
-def _result(t: Optional[torch.Tensor], like: torch.Tensor, shape, dtype: torch.dtype, name: str, dv: int, stream):
-    """A result of a call on ``stream`` (None: the current one) and its address:
-    the caller's tensor, checked, or a new one, whose memory is that stream's."""
-    if t is not None:
-        numel = 1
-        for n in shape:
-            numel *= n
-        return t, _at(t, dtype, name, dv, numel)
+def _new(like: torch.Tensor, shape, dtype: torch.dtype, stream) -> torch.Tensor:
+    """A result of a call on ``stream`` (None: the current one), whose memory is that
+    stream's."""
     if stream is None:
-        t = like.new_empty(shape, dtype=dtype)
-    else:
-        with torch.cuda.stream(stream):
-            t = like.new_empty(shape, dtype=dtype)
-    return t, t.data_ptr() or None
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _matrix(x: torch.Tensor, name: str):
-    if x.dim() != 2:
-        raise ValueError(f"{name} is {tuple(x.shape)}; it must be a matrix")
-    return x.shape
+def _rows(like: torch.Tensor, m: int, k: int, out, scales, dv: int, stream):
+    """Codes and scales of m rows, the caller's tensors or new ones, and their addresses."""
+    q = _new(like, (m, k), torch.int8, stream) if out is None else out
+    s = _new(like, (m,), torch.float32, stream) if scales is None else scales
+    qp = q.data_ptr() or None if out is None else _at(q, torch.int8, "out", dv, m * k)
+    return q, s, qp, s.data_ptr() or None if scales is None else _at(s, torch.float32, "scales", dv, m)
 
 
 def quantize_rows(x: torch.Tensor, out: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
                   stream=None) -> Rows:
     """Codes (int8 [m, k]) and scales (fp32 [m]) of the rows of ``x`` [m, k], bf16
     or fp32: scale = max |x| / 127, code = rint(x / scale)."""
-    (m, k), dv = _matrix(x, "x"), _device(x, "x")
-    if x.dtype not in _DT:
-        raise ValueError(f"x is {x.dtype}; it must be bf16 or fp32")
-    q, qp = _result(out, x, (m, k), torch.int8, "out", dv, stream)
-    s, sp = _result(scales, x, (m,), torch.float32, "scales", dv, stream)
-    N.check(N.lib.pgsr_quantize_rows_int8(m, k, _DT[x.dtype], _at(x, x.dtype, "x", dv, m * k), qp, sp,
+    m, k, dv = _matrix(x, "x")
+    dtype = x.dtype
+    if dtype not in _DT:
+        raise ValueError(f"x is {dtype}; it must be bf16 or fp32")
+    q, s, qp, sp = _rows(x, m, k, out, scales, dv, stream)
+    N.check(N.lib.pgsr_quantize_rows_int8(m, k, _DT[dtype], _at(x, dtype, "x", dv, m * k), qp, sp,
                                           _stream_ptr(stream, dv)))
     return q, s
 
@@ -77,9 +76,8 @@ def rmsnorm_int8(x: torch.Tensor, gain: torch.Tensor, eps: float, out: Optional[
                  scales: Optional[torch.Tensor] = None, stream=None) -> Rows:
     """``quantize_rows`` of x / sqrt(mean(x^2) + eps) * gain (bf16 ``x`` [m, k],
     ``gain`` [k]), with no rounding in between."""
-    (m, k), dv = _matrix(x, "x"), _device(x, "x")
-    q, qp = _result(out, x, (m, k), torch.int8, "out", dv, stream)
-    s, sp = _result(scales, x, (m,), torch.float32, "scales", dv, stream)
+    m, k, dv = _matrix(x, "x")
+    q, s, qp, sp = _rows(x, m, k, out, scales, dv, stream)
     N.check(N.lib.pgsr_rmsnorm_int8(m, k, _at(x, torch.bfloat16, "x", dv, m * k),
                                     _at(gain, torch.bfloat16, "gain", dv, k), eps, qp, sp, _stream_ptr(stream, dv)))
     return q, s
@@ -89,12 +87,11 @@ def silu_mul_int8(gate_up: torch.Tensor, out: Optional[torch.Tensor] = None, sca
                   stream=None) -> Rows:
     """``quantize_rows`` of SiLU(gate) * up for bf16 ``gate_up`` [m, 2 d_ff] (gate,
     then up), with no rounding in between."""
-    (m, k2), dv = _matrix(gate_up, "gate_up"), _device(gate_up, "gate_up")
+    m, k2, dv = _matrix(gate_up, "gate_up")
     if k2 % 2:
         raise ValueError(f"gate_up is {tuple(gate_up.shape)}; it must be [m, 2 d_ff]")
     k = k2 // 2
-    q, qp = _result(out, gate_up, (m, k), torch.int8, "out", dv, stream)
-    s, sp = _result(scales, gate_up, (m,), torch.float32, "scales", dv, stream)
+    q, s, qp, sp = _rows(gate_up, m, k, out, scales, dv, stream)
     N.check(N.lib.pgsr_silu_mul_int8(m, k, _at(gate_up, torch.bfloat16, "gate_up", dv, m * k2), qp, sp,
                                      _stream_ptr(stream, dv)))
     return q, s
@@ -102,7 +99,10 @@ def silu_mul_int8(gate_up: torch.Tensor, out: Optional[torch.Tensor] = None, sca
 
 def _weight(wq: torch.Tensor, ws: torch.Tensor, k: int, dv: int):
     """Rows of a weight, and the addresses of its codes and scales."""
-    n, k2 = _matrix(wq, "w")
+    shape = wq.shape
+    if len(shape) != 2:
+        raise ValueError(f"w is {tuple(shape)}; it must be a matrix")
+    n, k2 = shape
     if k2 != k:
         raise ValueError(f"w is {tuple(wq.shape)}; x has k = {k}")
     return n, _at(wq, torch.int8, "w", dv, n * k), _at(ws, torch.float32, "ws", dv, n)
@@ -113,9 +113,11 @@ def gemm_int8(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.Te
     """Y = (Xq Wq^T) * xs * ws (+ R), bf16: int8 codes ``xq`` [m, k], ``wq`` [n, k],
     fp32 scales of the tokens ``xs`` [m] and of the output channels ``ws`` [n]; the
     sums are exact.  ``r`` may be ``out``."""
-    (m, k), dv, bf = _matrix(xq, "x"), _device(xq, "x"), torch.bfloat16
+    m, k, dv = _matrix(xq, "x")
+    bf = torch.bfloat16
     n, wp, wsp = _weight(wq, ws, k, dv)
-    y, yp = _result(out, xq, (m, n), bf, "out", dv, stream)
+    y = _new(xq, (m, n), bf, stream) if out is None else out
+    yp = y.data_ptr() or None if out is None else _at(y, bf, "out", dv, m * n)
     N.check(N.lib.pgsr_gemm_int8(m, n, k, _at(xq, torch.int8, "x", dv, m * k), _at(xs, torch.float32, "xs", dv, m), wp, wsp,
                                  _at(r, bf, "r", dv, m * n) if r is not None else None, yp, _stream_ptr(stream, dv)))
     return y
@@ -125,7 +127,8 @@ def gemm_int8_multi(xq: torch.Tensor, xs: torch.Tensor, wqs: Sequence[torch.Tens
                     outs: Sequence[torch.Tensor], stream=None) -> Sequence[torch.Tensor]:
     """out_i = (Xq Wq_i^T) * xs * ws_i for up to three weights: the bits of one
     ``gemm_int8`` each, in one launch."""
-    (m, k), dv, c = _matrix(xq, "x"), _device(xq, "x"), len(wqs)
+    m, k, dv = _matrix(xq, "x")
+    c = len(wqs)
     if len(wss) != c or len(outs) != c:
         raise ValueError(f"{c} weights but {len(wss)} scales and {len(outs)} outputs")
     ns, wps, wsps, yps = [], [], [], []
