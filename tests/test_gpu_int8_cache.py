@@ -391,6 +391,29 @@ def test_fork_and_copy_on_write():
                 assert np.array_equal(a, b)
 
 
+def test_single_tokens_of_forked_sequences():
+    """Branches that share a partial block with their base and each other, re-decoded
+    with a workspace (the first step copies the block, the next append in the decode
+    kernel): as sequences that share nothing."""
+    geom = W.AttnGeometry(8, 2, 128)
+    rng = np.random.default_rng(41)
+    base = [_bf16(_rand(rng, 53, h, 128)) for h in (8, 2, 2)]
+    steps = [[_bf16(_rand(rng, 3, h, 128)) for h in (8, 2, 2)] for _ in range(14)]
+    shared, own = (_pool(geom, 40, 3, 8, split_q=3, max_splits=4) for _ in range(2))
+    assert shared.replay(0, [0], [53], *base, torch.empty_like(base[0]), 0.09) == 0
+    assert shared.fork([0, 0], [1, 2]) == 0
+    for i in range(3):
+        assert own.replay(0, [i], [53], *base, torch.empty_like(base[0]), 0.09) == 0
+    for n, x in enumerate(steps):
+        o = [torch.empty_like(x[0]) for _ in range(2)]
+        for pool, out in zip((shared, own), o):
+            assert pool.replay(0, [0, 1, 2], [1, 1, 1], *x, out, 0.09) == 0
+        assert torch.equal(o[0], o[1]), n
+        for s in range(3):
+            for a, b in zip(_stored(shared, 0, s, 54 + n), _stored(own, 0, s, 54 + n)):
+                assert np.array_equal(a, b), (n, s)
+
+
 def test_other_stream_and_captured_decode():
     """A decode step of two layers on a stream of its own, then recorded as a graph
     and replayed with other inputs and eager work between the replays."""

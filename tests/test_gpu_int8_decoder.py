@@ -77,6 +77,22 @@ def test_int8_decoder_matches_oracle_and_full_reset(hq, hkv, d, kv):
     assert off(_f64(out), plain) <= 0.04
 
 
+def test_wide_int8_layers_equal_the_full_reset():
+    """States of 4096 values: a suffix of 1 to 300 tokens takes other kernels of the
+    norm and the products than the whole session does, with the same bits."""
+    hq, hkv, d = 32, 8, 128
+    log("int8 decoder layer of 4096")
+    w, x, xc = _setup(hq, hkv, d, INT8, 5, T=700, P=1, Tc=720, dff=4112)[1:4]
+    mk = lambda: DecoderReplay(w[:1], hq, hkv, d, EPS, THETA, n_blocks=48, max_seqs=1, max_blocks_per_seq=48,  # noqa: E731
+                               kv_dtype=INT8)
+    full = mk().full_reset(0, _dev(x))
+    for S in (1, 40, 300):
+        dec = mk()
+        dec.replay(0, _dev(np.concatenate([x[:700 - S], xc[700 - S:]])))
+        assert dec.crop([0], [700 - S]) == 0
+        assert torch.equal(dec.replay(0, _dev(x[700 - S:])), full[700 - S:]), S
+
+
 @pytest.mark.parametrize("kv", [INT8, BF16])
 def test_int8_decoder_is_the_calls_it_is_made_of(kv):
     """The layers, written out in the public calls: the same bits."""
