@@ -327,10 +327,11 @@ int pgsr_pool_last_clock(pgsr_pool *pool, void *stream, double *ghz, int64_t *cy
  *  - other bf16 pools, FP8 and int8 pools: the software-pipelined kernel (32 query
  *    rows per wave, two waves per SIMD) or, for calls that leave CUs idle, with one
  *    wave per SIMD (FP8, int8) or the four-wave kernel (bf16);
- *  - int8 pools, calls that fill the chip and read every key in five tiles or more,
- *    with a workspace of 512 bytes per KV head and token and a table (4 bytes per 16
- *    tokens of the longest sequence, for each sequence): the wide kernel on a bf16
- *    copy of the call's keys and values that the workspace takes;
+ *  - int8 pools, calls that read every key in five or six tiles or more and fill the chip
+ *    or are split for it, with a workspace of 512 bytes per KV head and token and a table (4
+ *    bytes per 16 tokens of the longest sequence, for each sequence) beside the splits'
+ *    partials: the wide or narrow kernel on a bf16 copy of the call's keys and values that
+ *    the workspace takes;
  *  - the four-wave kernel for batches whose sequences fill the larger tiles badly
  *    (FP8, int8 and groups G = n_q_heads / n_kv_heads that do not divide 32), for
  *    calls with split keys of such groups in bf16, and for those of FP8 and int8

@@ -47,7 +47,9 @@
 // fetches 16, and the codes widen to bf16 exactly (every E4M3 value has at
 // most 4 significant bits) before the LDS store, so everything after the store
 // is the bf16 kernel.  The K scale rides in the softmax scale, the V scale in
-// the output normalisation.
+// the output normalisation.  Int8 cache: each code times the power of two of its
+// token and KV head, also exact in bf16; a thread's V chunks hold the same eight
+// keys, so that it reads and takes apart their exponents once.
 //
 // Key tiles sit at absolute positions and rows never interact, so a query's
 // output bits depend only on its absolute position and its own keys: selective

@@ -1,4 +1,4 @@
-// Prefix + causal prefill attention for head_dim 128 over a bf16 or FP8 cache
+// Prefix + causal prefill attention for head_dim 128 over a bf16, FP8 or int8 cache
 // on CDNA4 matrix cores (gfx950), software-pipelined so that each wave overlaps
 // its own matrix products with its own softmax arithmetic.
 //
@@ -8,7 +8,7 @@
 // one 32-row block of (token, head) query rows (the last rows are padding where
 // G does not divide 32), and the two waves of a SIMD interleave their matrix
 // products with each other's softmax arithmetic.  Three 35 KB LDS tile buffers
-// keep one workgroup per CU.  NW = 4 is for FP8 calls that leave CUs idle: half the
+// keep one workgroup per CU.  NW = 4 is for FP8 and int8 calls that leave CUs idle: half the
 // rows, a shorter step (32 query / 8 KV heads, 1024 tokens against 8189: 178 us,
 // eight waves 236, four-wave kernel 209).
 //
@@ -16,6 +16,10 @@
 // and the codes widen to bf16 exactly before the LDS store; the K scale rides
 // in scale_log2, the V scale in o_scale.  The 8B replay (2048 tokens against
 // 8189) takes 297 us against 316 with the four-wave kernel.
+// Int8 cache: each code times the power of two of its token is a bf16 value, three
+// instructions a code against one for FP8 (the same replay 337 us, FP8 284, four-wave
+// 385), so calls with a workspace whose keys are read by many tiles run on a bf16 copy
+// instead (276 us).
 // blockIdx.x = tile * n_kv_heads + g, so all tiles of a KV head land on one
 // XCD and share its L2 copy of the head's keys and values; tiles are issued
 // costliest first.

@@ -734,12 +734,15 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
     // FP8 calls whose larger tiles all have a CU (450 tokens: 51, pipelined 44).
     int narrow = 0, pipe = 0;       // waves per workgroup of the kernel taken
     bool wide = false;
-    // Int8 calls that fill the chip: their keys and values as bf16 in the workspace, if
-    // it has the room, and the wide kernel on those, with the same bits, where each key
-    // is read by five tiles or more: the pipelined kernel converts it in every one (us a
-    // call, 32 / 8 heads, pipelined and through the copy: 2048 tokens on 8189 338, 276;
-    // 2048 on none 86, 72; 64 / 8 heads, 8 x 200 on 3000, seven tiles 219, 195; 8 x 256
-    // on 4000, four 162, 164; 60 x 64 on 3000, one 250, 432).
+    // Int8: the call's keys and values as bf16 in the workspace, if it has the room, and
+    // the kernels of bf16 on those, with the same bits, where each key is read by five
+    // tiles or more: the pipelined kernel converts it in every one (us a call, pipelined
+    // and through the copy, 32 / 8 heads: 2048 tokens on 8189 338, 276; 2048 on none 86,
+    // 72; 64 / 8 heads, 8 x 200 on 3000, seven tiles 219, 195; 8 x 256 on 4000, four 162,
+    // 164; 60 x 64 on 3000, one 250, 432).  Split calls from six tiles on, whose larger
+    // tiles all have a CU (32 / 8 heads, 700 on 8189 177, 148; 1024 on 30000 610, 469; 512
+    // on 2000 49.6, 48.7; 64 / 8, five tiles on 8189 78.4, 83.9; 32 / 4, 400 on 8189, 260
+    // workgroups 101, 111).
     ExpandArgs x{};
     auto reused = [&] {
       const int tokens = attn_bf16_pipe_tile_tokens(group, 8);
@@ -749,12 +752,16 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
         steps += t * (chunk[i].prefix + 0.5 * chunk[i].q_len);
         keys += chunk[i].prefix + chunk[i].q_len;
       }
-      return steps >= 5 * keys;
+      return steps / keys;
     };
-    if (cache == kCacheInt8 && p->prefill_kind == PGSR_PREFILL_AUTO && a.n_splits == 1 && ws_bytes > 0 &&
-        !fits(attn_bf16_narrow_tile_tokens(group, 4)) && reused() && eight_pays(5, 0.75))
-      wide = plan_expand(p, a, ws, ws_bytes, x);
-    if (wide) {
+    bool copy = cache == kCacheInt8 && p->prefill_kind == PGSR_PREFILL_AUTO && ws_bytes > 0 &&
+                (a.n_splits > 1 ? 32 % group == 0 && fits(attn_bf16_pipe_tile_tokens(group, 8)) && reused() >= 6
+                                : !fits(attn_bf16_narrow_tile_tokens(group, 4)) && reused() >= 5 && eight_pays(5, 0.75));
+    if (copy) {
+      const size_t parts = a.n_splits > 1 ? (size_t)a.n_splits * a.n_rows * (p->d + 2) * sizeof(float) : 0;
+      copy = plan_expand(p, a, (char*)ws + parts, ws_bytes - parts, x);   // behind the splits' partials
+    }
+    if (copy) {
       hipError_t err = launch_expand_int8(x, st);
       if (err != hipSuccess) return hip_fail(err, "expand launch");
       a.k_cache = x.k_out;
@@ -765,6 +772,8 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
       a.block_size = 16;
       a.layer = 0;
       for (int32_t i = 0; i < cnt; ++i) a.e[i].seq = i;
+      narrow = a.n_splits > 1 && fits(attn_bf16_narrow_tile_tokens(group, 4)) ? 4 : 0;
+      wide = !narrow;
     } else if (p->dtype == PGSR_F32) {
       set_tiles(attn_f32_tile_tokens(p->d, group));
     } else if (wide_ok && (split_as_wide || a.n_splits == 1)) {

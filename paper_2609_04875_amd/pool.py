@@ -4,6 +4,9 @@
 (caches, block table, lengths, free-list stack, split workspace) and exposes
 the three calls of the hot path: ``crop`` (restore, Algorithm 1), ``replay``
 (the prefill form of the replay loop) and ``full_reset`` (baseline B5).
+
+An INT8 pool holds K and V as int8 codes under a power of two for each token and
+KV head (``kv_exponents``), quantised by the append; there is nothing to calibrate.
 """
 from __future__ import annotations
 
@@ -130,7 +133,7 @@ class KVPool:
         N.check(N.lib.pgsr_pool_set_kv_scales(self._h, ks, vs))
 
     def set_prefill_kernel(self, kind: str) -> None:
-        """Prefill kernel of a head_dim 128 bf16 or FP8 pool: "auto" (by size,
+        """Prefill kernel of a head_dim 128 bf16, FP8 or int8 pool: "auto" (by size,
         cache and block size), "pipelined" or "four_wave"; the same bits for calls
         with the same number of splits (without a workspace always)."""
         code = {"auto": 0, "four_wave": 1, "pipelined": 2}[kind]

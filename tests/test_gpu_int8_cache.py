@@ -66,6 +66,22 @@ def _decode_bound(q, k, v, pos0, scale, want):
     return 2.0 ** -8 * (mag + 2 * np.abs(want)) * 1.01 + 1e-5 * mag + 1e-30
 
 
+def _query_rounding(q, k, v, scale, o):
+    """The prefill kernels round a query times the scale to bf16, half a step: 2^-8 of
+    each of its values, so a score moves by d_j <= 2^-8 scale sum |q_i k_ij|, a weight
+    by a factor within e^(+-2 max d) of its own, and the result by at most
+    e^(2 max d) sum p_j d_j (|v_j| + |o|)."""
+    group, out = q.shape[0] // k.shape[1], np.zeros_like(o)
+    for h in range(q.shape[0]):
+        kh, vh = k[:, h // group], v[:, h // group]
+        s = kh @ q[h] * scale
+        p = np.exp(s - s.max())
+        d = 2.0 ** -8 * scale * (np.abs(kh) @ np.abs(q[h]))
+        w = p / p.sum() * d
+        out[h] = np.exp(2 * d.max()) * (w @ np.abs(vh) + w.sum() * np.abs(o[h]))
+    return out
+
+
 def _special_rows(x, at):
     """Rows that saturate, vanish, tie, hold zeros, infinities and subnormals."""
     x[at + 0, 0] = 0.0
@@ -497,6 +513,37 @@ def test_caches_past_32_bits():
                 assert pool.replay(0, [0], [len(x[0])], *x, outs[-1], 0.09) == 0
     assert int(far.block_tables[0, :120].min()) > 262144          # past 2^32 bytes of codes
     assert all(torch.equal(x, y) for x, y in zip(outs[:9], outs[9:]))
+
+
+@pytest.mark.parametrize("hq,hkv,B,P,S", [(32, 8, 16, 3000, 700), (32, 8, 32, 1990, 1024), (32, 4, 64, 2500, 250),
+                                          (16, 16, 16, 4001, 1500), (8, 2, 16, 900, 701)])
+def test_split_prefill_through_the_copy(hq, hkv, B, P, S):
+    """Calls with split keys on the bf16 copy behind the partials: the bits of the
+    pipelined kernel on the codes, of a pool whose workspace has no room for the copy,
+    and the oracle's values."""
+    from paper_2609_04875_amd import INT8, KVPool, workspace_bytes
+    log(f"int8 split prefill {hq}/{hkv} B={B} {S} on {P}")
+    geom, rng = W.AttnGeometry(hq, hkv, 128), np.random.default_rng(S)
+    z = [_bf16(_rand(rng, P, h, 128)) for h in (hq, hkv, hkv)]
+    x = [_bf16(_rand(rng, S, h, 128)) for h in (hq, hkv, hkv)]
+    copy = 512 * hkv * (P + S + 16) + 4 * (P + S)
+    outs = []
+    for splits, room, kind in ((8, 0, "pipelined"), (8, copy, "auto"), (8, copy, "pipelined")):
+        pool = KVPool(1, hq, hkv, 128, _blocks(P + S, B), 1, _blocks(P + S, B), INT8, B,
+                      workspace_bytes=workspace_bytes(hq, 128, S, splits) + room)
+        pool.set_prefill_kernel(kind)
+        assert pool.replay(0, [0], [P], *z, torch.empty_like(z[0]), 0.09) == 0
+        outs.append(torch.full_like(x[0], float("nan")))
+        assert pool.replay(0, [0], [S], *x, outs[-1], 0.09) == 0
+        torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    k, v = _read(pool, 0, 0, P + S)
+    rows = np.unique(np.r_[0, 1, S - 1, rng.integers(0, S, 12)])
+    for i in rows:
+        q = _f64(x[0][i:i + 1])
+        want = oracle.attention(q, k[:P + i + 1], v[:P + i + 1], P + int(i), 0.09)
+        assert (np.abs(_f64(outs[1][i:i + 1]) - want) <= _decode_bound(q, k[:P + i + 1], v[:P + i + 1], P + int(i), 0.09, want)
+                + _query_rounding(q[0], k[:P + i + 1], v[:P + i + 1], 0.09, want[0])).all()
 
 
 def test_captured_prefill_through_the_copy():
