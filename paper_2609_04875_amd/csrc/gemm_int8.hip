@@ -17,9 +17,10 @@
 // of rows: against four waves that split the outputs, 1 x 3584 x 18944 17.2 -> 12.4 us,
 // 1 x 28672 x 4096 22.8 -> 19.5, 102 x 4096 x 14336 24.4 -> 23.7, 200 rows 30.3 -> 28.5.
 // Few rows stream W from HBM once.  From 64 rows on what bounds it is the lines that a
-// CU can have on their way: some 110 of 128 bytes, each 490 cycles on average where a
-// quarter come from HBM (102 x 3584 x 18944: 76 GB/s a CU, 125 with every line in L2),
-// so larger tiles pay as soon as they fill the CUs, and LDS or the products do not.
+// CU can have on their way: about 100 of 128 bytes, each 370 to 490 cycles on average
+// where a quarter come from HBM (102 x 3584 x 18944: 70 GB/s a CU; 125 with every line
+// in L2), so larger tiles pay as soon as they fill the CUs, and LDS or the products do
+// not.
 //
 // K any multiple of 16: the last stage clamps the chunks past K to the row's last
 // one, and their operands of X are cleared in registers (W's may hold anything:
