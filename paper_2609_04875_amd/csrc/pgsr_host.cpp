@@ -285,8 +285,8 @@ constexpr int32_t kDecodeMinSplitKeys = PGSR_DECODE_MIN_SPLIT_KEYS;
 
 // Tiles per split of a decode launch over `kv` keys per sequence, at most `most`
 // splits to a sequence and `row_bytes` to a cached key; the longest sequence's
-// tiles when it is not cut.
-int64_t decode_split_tiles(const std::vector<int64_t>& kv, int64_t hkv, int64_t most, int64_t row_bytes) {
+// tiles when it is not cut.  `int8`: an int8 pool's.
+int64_t decode_split_tiles(const std::vector<int64_t>& kv, int64_t hkv, int64_t most, int64_t row_bytes, bool int8) {
   const int64_t kt = attn_decode_keys_per_tile(), n = (int64_t)kv.size();
   const int64_t max_key = *std::max_element(kv.begin(), kv.end());
   const int64_t whole = cdiv(max_key, kt);
@@ -297,7 +297,12 @@ int64_t decode_split_tiles(const std::vector<int64_t>& kv, int64_t hkv, int64_t 
   // from 550 (FP8, 4 KV heads) to 800 (bf16, 8 KV heads).  64 x 400 keys bf16: 37 us
   // whole, 44 cut; 8 x 400: 23 and 15.
   const double heavy = (double)(n * hkv * row_bytes) / (512.0 * 256.0);
-  const double line = 5.0 + (double)n / (row_bytes >= 256 ? 8.0 : 5.0) + 12.0 * heavy * heavy * heavy;
+  // The splits of int8 pools are joined in half the time, and few sequences gain from
+  // five tiles on (GPU us cut and whole, 8 KV heads: one of 128 keys 8.9, 12.1, of 96
+  // 10.0, 10.8, but a launch more for the host; 32 x 200 10.4, 15.2; 60 x 160 15.1, 14.0,
+  // 60 x 320 17.5, 20.7; 4 KV heads, 60 x 512 17.8, 28.6).
+  const double line = int8 ? 4.0 + 34.0 * heavy * heavy * heavy
+                           : 5.0 + (double)n / (row_bytes >= 256 ? 8.0 : 5.0) + 12.0 * heavy * heavy * heavy;
   if (most <= 1 || (double)whole <= line) return whole;
   auto shortest = [&](int64_t target) {
     int64_t hi = whole;
@@ -639,7 +644,7 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
       const int64_t max_key = *std::max_element(kv.begin(), kv.end());
       const int64_t per_split = (int64_t)a.n_rows * ((int64_t)p->d + 2) * (int64_t)sizeof(float);
       const int64_t most = std::min<int64_t>(kDecodeMaxSplits, (int64_t)(ws_bytes / std::max<int64_t>(per_split, 1)));
-      const int64_t len = decode_split_tiles(kv, p->hkv, most, (int64_t)p->d * eb) * attn_decode_keys_per_tile();
+      const int64_t len = decode_split_tiles(kv, p->hkv, most, (int64_t)p->d * eb, cache == kCacheInt8) * attn_decode_keys_per_tile();
       a.n_splits = cdiv(max_key, len);
       if (a.n_splits > 1) {
         a.split_len = (int32_t)len;
