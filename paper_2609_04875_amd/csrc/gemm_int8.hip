@@ -213,33 +213,36 @@ void launch_tile(const Int8Args& a, hipStream_t s) {
 // Tile choice: the time of a launch is close to
 //   max(1, 0.36 r + 0.64 ceil(r)) * (K / 128 * step + fix),   r = tiles / 256 CUs
 // (a partly filled last round costs most of a whole one): one 128-k step of one tile
-// per CU, and a tile's prologue and epilogue.  step and fix are fitted to 311 products
-// (M 1 to 4096; N and K of three models' projections and smaller ones, W out of the
-// caches), where the tile it picks is 0.6% slower than the fastest of the eleven on
-// average and 12% at most (1 x 8192 x 28672 in 32 x 32 tiles 42.3 us, 16 x 16 37.9).
-// 16 x 16 tiles in number run rings of two stages, five workgroups to a CU (1 x 28672 x
-// 4096 19.5 us, four stages 22.3; 1 x 57344 x 8192 66.1, 68.5), few of them four (1 x
-// 3584 x 18944 12.4 us, two stages 16.5; 1 x 8192 x 28672 37.7, 40.7).
+// per CU, and a tile's prologue and epilogue.  step and fix are fitted to 494 products
+// (M 1 to 6000; N and K of three models' projections, W out of the caches, and drawn
+// ones from 8 and 16 on), where the tile it picks is 0.5% slower than the fastest of the
+// eleven on average and 18% at most (32 x 6144 x 4096 in 32 x 32 tiles 9.3 us, 16 x 16
+// 7.9).  A wave of 16 x 16 tiles has a ring of four stages where they are few, two
+// workgroups to a CU, and K is long or W large enough to come from HBM (1 x 3584 x 18944
+// 12.4 us, two stages 16.5; 1 x 32 x 11904 7.3, 10.0), of two else, five to a CU (1 x
+// 28672 x 4096 19.5 us, four stages 22.3; 83 x 416 x 3456 4.1, 4.4).
 struct TileCost {
   int bm, bn;
   double step_ns, fix_ns;
 };
-constexpr TileCost kTiles[] = {{16, 16, 57, 888},     {16, 16, 50, 494},     {32, 16, 60, 683},    {32, 32, 103, 858},
-                               {64, 32, 150, 2129},   {64, 64, 265, 2478},   {128, 64, 354, 1809}, {128, 128, 588, 1730},
-                               {256, 128, 920, 2537}, {256, 128, 863, 3144}, {256, 256, 1529, 2340}};
-constexpr int kDeep = 0, kShallow = 1; // 16 x 16 by the number of tiles
-constexpr int kManyTiles = 4 * kCus;
+constexpr TileCost kTiles[] = {{16, 16, 50, 826},      {16, 16, 54, 391},     {32, 16, 60, 724},    {32, 32, 103, 858},
+                               {64, 32, 184, 1686},    {64, 64, 238, 3067},   {128, 64, 354, 1809}, {128, 128, 582, 1585},
+                               {256, 128, 1051, 1148}, {256, 128, 863, 3144}, {256, 256, 1529, 2340}};
+constexpr int kDeep = 0, kShallow = 1; // 16 x 16
+constexpr int kDeepK = 8192;
+constexpr double kDeepBytes = 8e6;
 constexpr int kWide = 9;               // from here on gemm_int8_wide.hip: K a multiple of 128
 
 int pick_tile(int m, int k, int count, const int* n) {
   int best = -1;
-  double best_cost = 0;
+  double best_cost = 0, bytes = 0;
+  for (int j = 0; j < count; ++j) bytes += (double)n[j] * k;
   for (int i = 0; i < (k % 128 == 0 ? kWide + 2 : kWide); ++i) {
     const TileCost& t = kTiles[i];
     double cols = 0;
     for (int j = 0; j < count; ++j) cols += ((int64_t)n[j] + t.bn - 1) / t.bn;
     const double tiles = (double)(((int64_t)m + t.bm - 1) / t.bm) * cols, r = tiles / kCus;
-    if (i == (tiles > kManyTiles ? kDeep : kShallow)) continue;
+    if (i <= kShallow && (i == kDeep) != (tiles <= 2 * kCus && (k >= kDeepK || bytes >= kDeepBytes))) continue;
     if (tiles * 512 >= 4294967296.0) continue;     // a launch counts its threads in 32 bits
     const double cost = (r <= 1.0 ? 1.0 : 0.36 * r + 0.64 * ceil(r)) * ((k + 127) / 128 * t.step_ns + t.fix_ns);
     if (best < 0 || cost < best_cost) {
