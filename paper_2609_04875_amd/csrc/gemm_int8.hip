@@ -8,7 +8,7 @@
 // conversion to fp32 rounds sums past 2^24 by half a step of fp32.  Integer sums have no
 // order, so a result depends on no tile, and rows not on which rows share the launch.
 //
-// This file: the choice of the tile, and the kernel of tiles from 16 x 16 to 64 x 64.
+// This file: the choice of the tile, and the kernel of tiles from 16 x 16 to 96 x 64.
 // Its four waves share the tile's outputs and split K: wave w takes the 128-k stages
 // w, w + 4, ... through a ring of its own in LDS (global->LDS loads: a request is 8 rows
 // x 128 bytes, chunk c of row j in slot c ^ ((j / 2) mod 8)), waits for its own requests
@@ -16,6 +16,7 @@
 // the loop, each byte read from LDS once, and four stages of K at a time from a handful
 // of rows: against four waves that split the outputs, 1 x 3584 x 18944 17.2 -> 12.4 us,
 // 1 x 28672 x 4096 22.8 -> 19.5, 102 x 4096 x 14336 24.4 -> 23.7, 200 rows 30.3 -> 28.5.
+// (96 x 64, all of the LDS: 316 rows 34.1, the ring of 128 x 64 tiles 41.5.)
 // Few rows stream W from HBM once.  From 64 rows on what bounds it is the lines that a
 // CU can have on their way: about 100 of 128 bytes, each 370 to 490 cycles on average
 // where a quarter come from HBM (102 x 3584 x 18944: 70 GB/s a CU; 125 with every line
@@ -213,11 +214,11 @@ void launch_tile(const Int8Args& a, hipStream_t s) {
 // Tile choice: the time of a launch is close to
 //   max(1, 0.36 r + 0.64 ceil(r)) * (K / 128 * step + fix),   r = tiles / 256 CUs
 // (a partly filled last round costs most of a whole one): one 128-k step of one tile
-// per CU, and a tile's prologue and epilogue.  step and fix are fitted to 494 products
+// per CU, and a tile's prologue and epilogue.  step and fix are fitted to 602 products
 // (M 1 to 6000; N and K of three models' projections, W out of the caches, and drawn
 // ones from 8 and 16 on), where the tile it picks is 0.5% slower than the fastest of the
-// eleven on average and 18% at most (32 x 6144 x 4096 in 32 x 32 tiles 9.3 us, 16 x 16
-// 7.9).  A wave of 16 x 16 tiles has a ring of four stages where they are few, two
+// twelve on average and 13% at most (64 x 6144 x 4096 in 64 x 32 tiles 10.2 us, 32 x 32
+// 9.2).  A wave of 16 x 16 tiles has a ring of four stages where they are few, two
 // workgroups to a CU, and K is long or W large enough to come from HBM (1 x 3584 x 18944
 // 12.4 us, two stages 16.5; 1 x 32 x 11904 7.3, 10.0), of two else, five to a CU (1 x
 // 28672 x 4096 19.5 us, four stages 22.3; 83 x 416 x 3456 4.1, 4.4).
@@ -225,13 +226,13 @@ struct TileCost {
   int bm, bn;
   double step_ns, fix_ns;
 };
-constexpr TileCost kTiles[] = {{16, 16, 50, 826},      {16, 16, 54, 391},     {32, 16, 60, 724},    {32, 32, 103, 858},
-                               {64, 32, 184, 1686},    {64, 64, 238, 3067},   {128, 64, 354, 1809}, {128, 128, 582, 1585},
-                               {256, 128, 1051, 1148}, {256, 128, 863, 3144}, {256, 256, 1529, 2340}};
+constexpr TileCost kTiles[] = {{16, 16, 54, 892},   {16, 16, 50, 380},      {32, 16, 63, 719},     {32, 32, 99, 788},
+                               {64, 32, 164, 1921}, {64, 64, 218, 3230},    {96, 64, 319, 2763},   {128, 64, 354, 1809},
+                               {128, 128, 582, 1585}, {256, 128, 1051, 1148}, {256, 128, 863, 3144}, {256, 256, 1529, 2340}};
 constexpr int kDeep = 0, kShallow = 1; // 16 x 16
 constexpr int kDeepK = 8192;
 constexpr double kDeepBytes = 8e6;
-constexpr int kWide = 9;               // from here on gemm_int8_wide.hip: K a multiple of 128
+constexpr int kWide = 10;               // from here on gemm_int8_wide.hip: K a multiple of 128
 
 int pick_tile(int m, int k, int count, const int* n) {
   int best = -1;
@@ -261,9 +262,10 @@ hipError_t run_tile(int tile, const Int8Args& a, hipStream_t s) {
     case 3: launch_tile<32, 32, 2>(a, s); break;
     case 4: launch_tile<64, 32, 3>(a, s); break;
     case 5: launch_tile<64, 64, 2>(a, s); break;
-    case 6:
+    case 6: launch_tile<96, 64, 2>(a, s); break;
     case 7:
-    case 8: return launch_gemm_int8_ring(a, kTiles[tile].bm, kTiles[tile].bn, s);
+    case 8:
+    case 9: return launch_gemm_int8_ring(a, kTiles[tile].bm, kTiles[tile].bn, s);
     default: return launch_gemm_int8_wide(a, kTiles[tile].bn, s);
   }
   return hipGetLastError();

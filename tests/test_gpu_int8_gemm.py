@@ -181,7 +181,7 @@ PRODUCTS = [(1, 8, 16), (1, 4096, 4096), (2, 1024, 144), (3, 16, 32), (16, 24, 4
             (300, 4104, 4112), (333, 1000, 1232), (1000, 1000, 1008), (1025, 2048, 2064), (2048, 4096, 512),
             (2049, 4104, 528), (4096, 8192, 1024), (4100, 8200, 656), (70000, 8, 16), (5, 128256, 64), (1, 8, 133136),
             (9, 20008, 4112), (40, 200, 8208), (201, 3592, 1168), (700, 8200, 1152), (2049, 2056, 2176), (16, 16392, 1024),
-            (7, 3592, 18960), (27, 3592, 2064), (190, 4104, 2064), (33, 4104, 8208)]
+            (7, 3592, 18960), (27, 3592, 2064), (190, 4104, 2064), (33, 4104, 8208), (280, 3592, 8208)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)

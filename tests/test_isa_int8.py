@@ -14,7 +14,7 @@ import test_isa_inline_asm as base
 # source, kernel name, instantiations, requests of the smallest one (the prologue's and the loop's tiles)
 KERNELS = {"gemm_int8_wide": ("gemm_int8_wide.hip", "gemm_int8_wide_kernel", 2, 32),
            "gemm_int8_ring": ("gemm_int8_ring.hip", "gemm_int8_ring_kernel", 6, 6),
-           "gemm_int8": ("gemm_int8.hip", "gemm_int8_kernel", 12, 12)}
+           "gemm_int8": ("gemm_int8.hip", "gemm_int8_kernel", 14, 12)}
 
 
 @pytest.fixture(scope="module", params=sorted(KERNELS))
