@@ -692,6 +692,25 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
       const bool down = cache == kCacheInt8 && p->d == 128;
       int64_t ns = std::min<int64_t>(kMaxSplits, (target + (down ? 0 : wgs - 1)) / wgs);
       ns = std::min<int64_t>(ns, (int64_t)(ws_bytes / std::max<int64_t>(per_split, 1)));
+      // Of these int8 calls take as many as pay: 1.8 us for each 64-key tile of a split's
+      // walk against 2 us for the combine and the partials' way to memory and back (us a
+      // call with all and none: 64 / 8 heads, 4 x 120 tokens on 30 35, 17; 28 / 4, 8 x 120
+      // on 30 31, 18; 32 / 8, 4 x 40 on 1000 25, 42, in four 24).  249 calls are 2% slower
+      // than in their best number, 10% in as many as there is room for.
+      if (cache == kCacheInt8) {
+        const int64_t tiles = cdiv(max_key, kSplitAlign);
+        double least = 1.8 * (double)tiles;
+        int64_t best = 1;
+        for (int64_t i = 2; i <= ns; ++i) {
+          const int64_t walk = cdiv(tiles, i);
+          const double us = 1.8 * (double)walk + 2.0 + 2.5e-6 / 4.0 * (double)(cdiv(tiles, walk) * per_split);
+          if (us < least) {
+            least = us;
+            best = i;
+          }
+        }
+        ns = best;
+      }
       if (ns > 1) {
         const int32_t len = cdiv(cdiv(max_key, ns), kSplitAlign) * kSplitAlign;
         a.n_splits = cdiv(max_key, len);
@@ -737,6 +756,13 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
     // 126 tokens on 1600: 38.7 us, wide 50.7; 400 tokens on 900, narrow 35.4
     // against 31.2; FP8, 32 / 16 heads, 300 tokens on 2000 45, pipelined 51) but for
     // FP8 calls whose larger tiles all have a CU (450 tokens: 51, pipelined 44).
+    // Int8 calls that leave CUs idle and walk few keys take the four-wave kernel, which
+    // starts 1.7 us earlier and takes a tenth longer a tile (32 / 8 heads, 9 tokens on 10
+    // 10.6, pipelined 12.1 us; 60 on 400 in one split 25.4, 24.6; on 1000 42.3, 40.8).
+    int64_t walk = a.n_splits > 1 ? a.split_len / kSplitAlign : 0;
+    for (int32_t i = 0; i < cnt && a.n_splits == 1; ++i)
+      walk = std::max<int64_t>(walk, cdiv((int64_t)chunk[i].prefix + chunk[i].q_len, kSplitAlign));
+    const bool brief = cache == kCacheInt8 && walk < 10;
     int narrow = 0, pipe = 0;       // waves per workgroup of the kernel taken
     bool wide = false;
     // Int8: the call's keys and values as bf16 in the workspace, if it has the room, and
@@ -788,8 +814,8 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
       wide = narrow == 0 && (32 % group == 0 || eight_pays(5, 0.75));
     } else if (pipe_ok && (f8 || split_as_wide || a.n_splits == 1)) {
       if (p->prefill_kind == PGSR_PREFILL_PIPELINED) pipe = 8;
-      else if (fits(attn_bf16_pipe_tile_tokens(group, 4))) pipe = f8 ? 4 : 0;
-      else if (a.n_splits > 1) pipe = !f8 || fits(attn_bf16_pipe_tile_tokens(group, 8)) ? 8 : 0;
+      else if (fits(attn_bf16_pipe_tile_tokens(group, 4))) pipe = f8 && !brief ? 4 : 0;
+      else if (a.n_splits > 1) pipe = !f8 || (fits(attn_bf16_pipe_tile_tokens(group, 8)) && !brief) ? 8 : 0;
       else pipe = (!f8 && 32 % group == 0) || eight_pays(f8 ? 5 : 4, f8 ? 0.8 : 0.85) ? 8 : 0;
     }
     if (p->dtype != PGSR_F32)
