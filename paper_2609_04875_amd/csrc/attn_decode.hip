@@ -442,17 +442,18 @@ attn_decode_kernel(AttnArgs a, const int32_t* __restrict__ tables, const uint16_
   }
 }
 
-// Joins the splits of an int8 decode call: a wave for each query row.  Its partials, a
-// lane's four columns of every SPI-th split, are asked for at once, with the maxima and
-// sums (lane s: split s) and the entries, so the wave waits for memory once, where the
-// combine of the other pools, whose order of sums they keep, waits three to five times
-// (1331 keys in 21 splits 3.1 against 5.2 us, 40 ragged sequences 4.8 against 6.4).
-// Joining in the decode kernel itself, by the last wave of a sequence and KV head to
-// write, saves the launch and loses more: the partials then have to pass the caches of
-// the XCDs (32 x 8192 keys 103 us with device-scope accesses, 193 with fences, where the
-// two launches take 95 and 4.7; one sequence 17.4 against 10.4).
-// Splits past the row's own sequence hold older data and are left out.  A group of lanes
-// adds its splits in ascending order, then the groups are added: a fixed order.
+// Joins the splits of an int8 call (decode; prefill of few rows of head_dim 64): a wave
+// for each query row.  Its partials, a lane's four columns of every SPI-th split, are
+// asked for at once, with the maxima and sums (lane s: split s) and the entries, so the
+// wave waits for memory once, where the combine of the other pools, whose order of sums
+// they keep, waits three to five times (1331 keys in 21 splits 3.1 against 5.2 us, 40
+// ragged sequences 4.8 against 6.4).  Joining in the decode kernel itself, by the last
+// wave of a sequence and KV head to write, saves the launch and loses more: the partials
+// then have to pass the caches of the XCDs (32 x 8192 keys 103 us with device-scope
+// accesses, 193 with fences, where the two launches take 95 and 4.7; one sequence 17.4
+// against 10.4).  Splits past the row's own position hold older data and are left out.
+// A group of lanes adds its splits in ascending order, then the groups are added: a
+// fixed order.
 template <int D, int NI>
 __global__ void __launch_bounds__(256) join_splits_kernel(AttnArgs a, uint16_t* __restrict__ og) {
   constexpr int LPR = D / 4, SPI = 64 / LPR;
@@ -469,7 +470,7 @@ __global__ void __launch_bounds__(256) join_splits_kernel(AttnArgs a, uint16_t* 
   const int tok = row / a.n_q_heads;
   const uint64_t in = __ballot(lane < a.n && tok >= mine.q_off && tok < mine.q_off + mine.q_len);
   if (in == 0) return;                             // a row of no entry of this launch
-  const int ns = __builtin_amdgcn_readlane((mine.prefix + mine.q_len - 1) / a.split_len + 1, __builtin_ctzll(in));
+  const int ns = __builtin_amdgcn_readlane((mine.prefix + tok - mine.q_off) / a.split_len + 1, __builtin_ctzll(in));
   float M = lane < ns ? ml[0] : -INFINITY;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));

@@ -313,7 +313,7 @@ struct DecodeAppend {
 // `cache`: kCacheBf16, kCacheFp8 or kCacheInt8 (attn_common.h).
 hipError_t launch_attn_decode(const AttnArgs& a, int cache, const DecodeAppend& f, hipStream_t s);
 int attn_decode_keys_per_tile();
-// The combine of an int8 decode call (at most 64 splits): one round through memory.
+// The combine of an int8 call of few rows (at most 64 splits): one round through memory.
 hipError_t launch_join_splits(const AttnArgs& a, hipStream_t s);
 // Merge split-key partials into O (bf16, or fp32 for fp32 pools), splits in
 // increasing order, `group` (8 or 16) of them to a round trip.

@@ -836,7 +836,14 @@ int do_replay(pgsr_pool* p, int32_t layer, int32_t n, const int32_t* seqs,
                      : cache == kCacheFp8  ? launch_attn_fp8(a, st)
                      : cache == kCacheInt8 ? launch_attn_int8(a, st)
                                           : launch_attn_bf16(a, st);
-    if (err == hipSuccess && a.n_splits > 1) err = launch_split_combine(a, p->dtype == PGSR_F32, p->dtype == PGSR_F32 ? 16 : 8, st);
+    // Int8, head_dim 64 and few rows: the decode calls' join, a wave for each (8 heads, us a
+    // call joined and combined: 300 tokens on 1000 15.6, 18.4; 4 x 120 on 3000 23.8, 28.9; 4
+    // x 300 on 400 24.5, 23.5; 4 x 700 on 400 41.1, 36.7; head_dim 128, 32 heads, 120 on
+    // 1000 25.6, 20.6).
+    const bool join = cache == kCacheInt8 && p->d == 64 && a.row_end - a.row_begin < 4096;
+    if (err == hipSuccess && a.n_splits > 1)
+      err = join ? launch_join_splits(a, st)
+                 : launch_split_combine(a, p->dtype == PGSR_F32, p->dtype == PGSR_F32 ? 16 : 8, st);
     if (err != hipSuccess) return hip_fail(err, "attention launch");
   }
 

@@ -546,6 +546,39 @@ def test_split_prefill_through_the_copy(hq, hkv, B, P, S):
                 + _query_rounding(q[0], k[:P + i + 1], v[:P + i + 1], 0.09, want[0])).all()
 
 
+@pytest.mark.parametrize("hq,hkv,d,B,P,S", [
+    (8, 8, 64, 32, (2100, 700, 1500), (40, 120, 65)), (8, 2, 64, 16, (1000, 0, 3000), (300, 64, 170)),
+    (16, 4, 64, 64, (2600,), (37,)), (28, 4, 128, 16, (2100, 900), (12, 40)), (32, 8, 128, 64, (3001,), (9,)),
+    (8, 8, 64, 16, (700, 650), (300, 280))])
+def test_split_prefill_matches_the_oracle(hq, hkv, d, B, P, S):
+    """Prefill calls with split keys, few rows (joined by a wave each at head_dim 64) and
+    more, over a workspace of NaN: every partial that is read was written by the call."""
+    log(f"int8 split prefill {hq}/{hkv}/{d} B={B} {S} on {P}")
+    geom, rng, n = W.AttnGeometry(hq, hkv, d), np.random.default_rng(P[0] + S[0]), len(P)
+    pool = _pool(geom, sum(_blocks(p + s, B) for p, s in zip(P, S)), n, max(_blocks(p + s, B) for p, s in zip(P, S)), B,
+                 split_q=sum(S), max_splits=16)
+    for i, p in enumerate(P):
+        z = [_bf16(_rand(rng, p, h, d)) for h in (hq, hkv, hkv)]
+        assert pool.replay(0, [i], [p], *z, torch.empty_like(z[0]), 0.1) == 0
+    x = [_bf16(_rand(rng, sum(S), h, d)) for h in (hq, hkv, hkv)]
+    o = [torch.full_like(x[0], float("nan")) for _ in range(2)]
+    for out in o:
+        pool.workspace.fill_(0xFF)
+        assert pool.replay(0, list(range(n)), S, *x, out, 0.1, commit=out is o[1]) == 0
+        torch.cuda.synchronize()
+    assert torch.equal(o[0], o[1]) and (pool.workspace[:1024] != 0xFF).any()        # there were splits
+    off = 0
+    for i, (p, s) in enumerate(zip(P, S)):
+        k, v = _read(pool, 0, i, p + s)
+        for t in np.unique(np.r_[0, s - 1, rng.integers(0, s, 6)]):
+            q = _f64(x[0][off + t:off + t + 1])
+            kk, vv = k[:p + t + 1], v[:p + t + 1]
+            want = oracle.attention(q, kk, vv, p + int(t), 0.1)
+            bound = _decode_bound(q, kk, vv, p + int(t), 0.1, want) + _query_rounding(q[0], kk, vv, 0.1, want[0])
+            assert (np.abs(_f64(o[0][off + t:off + t + 1]) - want) <= bound).all(), (i, t)
+        off += s
+
+
 def test_captured_prefill_through_the_copy():
     """A long suffix recorded with its copy in the workspace, replayed with other
     inputs and eager calls that use the same workspace in between."""
